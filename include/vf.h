@@ -335,6 +335,107 @@ int vf_reuse_pool_extend(vf_reuse_pool *p, int32_t *drafts_host, int n_fresh);
 int vf_draft_suffix_match(const int32_t *history_host, int n, int max_suffix, int min_suffix, int k,
                           int32_t *drafts_host);
 
+/* ---- packed batches over the page pool (next to the three operations) ------------------------ */
+
+/* Three operators for a serving step of many requests whose rows are packed one behind the other:
+ * pages for the step's tokens, the rotary embedding with the write to the cache, and attention of all
+ * rows over the cache.  They need no model handle and no sequence handles, take lengths and offsets
+ * from device memory and work on one layer of a page pool: `kv_layer_dev` is the address of
+ *     T kv[pool_pages][2][n_kv_heads][64 * head_dim]        (0: K, 1: V; T by dtype)
+ * which for layer l of a pool of vf_kv_bytes(m, 64, n) bytes lies l * (bytes / n_layers) behind its
+ * start.  Inside a page and head the elements lie in the order the matrix instructions read them:
+ *     K: [32-key tile][half h][d / 32][d % 32 / 8][u][r][d % 8]          key = 32 * tile + 8 * u + 4 * h + r
+ *     V: [32-key tile][d / 16][key % 32 / 8][d % 16][key % 8]
+ * head_dim is 64 or 128.  A row is a token of the step; sequence b has the rows row_off[b] ..
+ * row_off[b + 1] - 1, which are the last tokens of its cache.  Device arrays that a call reads must not
+ * overlap those it writes, unless stated.  What the host cannot see is checked on the device: a page id outside the
+ * pool, an offset outside the rows or a position outside the table is never used as an address. */
+#define VF_PACKED_MAX_SEQS 4096      /* sequences of a call */
+#define VF_PACKED_MAX_ROWS (1 << 20)  /* rows of a call      */
+
+/* Pages for the tokens of a step.  Sequence b holds len[b] tokens in the pages block_table[b][0 ..
+ * ceil(len[b] / 64)) and gets new[b] more.  The pages it lacks come off the end of the free list
+ * free_pages[0 .. n_free), in the order of the sequences, and are entered into its table (row b at
+ * block_table_dev + b * table_stride, max_pages entries); nothing else of the table is written.
+ * A sequence is refused, and keeps what it had, if a length is negative, if it would pass 64 * max_pages
+ * tokens, or if it lacks pages and those before it (refused for want of pages or not) and itself lack more
+ * than n_free together.
+ *   row_off[n_seqs + 1]  offsets of the sequences' rows, in steps of new[b] (a refused sequence has its
+ *                        rows too), none above total_rows
+ *   pos[total_rows]      position of the row's token; -1: refused, or behind the last sequence's rows
+ *   slot[total_rows]     64 * page + place in the page; -1 as above, or if the table has no such page
+ *   kv_len[n_seqs]       len[b] + new[b]; 0 if refused
+ *   n_free_out[1]        entries left in the free list (its last ones were taken)
+ * total_rows = the sum of new[b] as the host knows it (0 allowed); free_entries = room of free_pages
+ * (n_free is taken as at most that). */
+int vf_pages_assign(int n_seqs, int max_pages, int table_stride, int total_rows, int free_entries,
+                    const int32_t *len_dev, const int32_t *new_dev, const int32_t *free_pages_dev,
+                    const int32_t *n_free_dev, int32_t *block_table_dev, int32_t *row_off_dev,
+                    int32_t *pos_dev, int32_t *slot_dev, int32_t *kv_len_dev, int32_t *n_free_out_dev,
+                    void *stream);
+
+#define VF_ROTARY_HALF         0  /* pairs (i, i + rotary_dim / 2)                                */
+#define VF_ROTARY_INTERLEAVED  1  /* pairs (2 i, 2 i + 1)                                          */
+#define VF_ROTARY_UNSCALED     0
+#define VF_ROTARY_POSITIONS    1  /* f_i / factor: positions are divided by it                     */
+#define VF_ROTARY_BASE         2  /* theta * factor^(rotary_dim / (rotary_dim - 2)): the slowest pair turns factor times slower */
+#define VF_ROTARY_RAMP         3  /* f_i * (g + (1 - g) / factor), g = clamp((n_i - low) / (high - low), 0, 1), */
+                                  /* n_i = trained * f_i / 2 pi: turns of pair i over the trained length */
+
+/* Rotary angles, f_i = theta^(-2 i / rotary_dim), i < rotary_dim / 2, changed as `scaling` says.
+ * rotary_dim is a multiple of 16 of at most 128; fields a scaling does not name are not read. */
+typedef struct {
+    int32_t rotary_dim, max_positions, scaling, pad;
+    double theta, factor, low, high, trained;
+    double magnitude;              /* multiplies cos and sin (1: plain rotation)              */
+} vf_rotary_plan;
+
+/* table_dev[max_positions][rotary_dim / 2][2] = (cos, sin) of position * f_i, float32; angles in float64. */
+int vf_rotary_table(const vf_rotary_plan *plan, float *table_dev, void *stream);
+
+typedef struct {
+    int32_t dtype, n_q_heads, n_kv_heads, head_dim;
+    int32_t rotary_dim, pairs;     /* VF_ROTARY_HALF | VF_ROTARY_INTERLEAVED                  */
+    int32_t total_rows, max_positions, pool_pages, pad;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;   /* elements between rows            */
+} vf_rotary_args;
+
+/* Rotates q and k by the angles of pos[row], the first rotary_dim elements of every head (the others stay), and puts
+ * q into q_out[row] (q itself allowed, with the same stride), k and v into the cache at slot[row].  Rows may be
+ * columns of wider matrices (strides); addresses and strides are multiples of 16 bytes.  Products and sums are
+ * float32, rounded once.  A row whose position is not in [0, max_positions) gets q_out = 0 and is not stored; one
+ * whose slot is not in [0, 64 * pool_pages) is not stored.  No two rows share a slot. */
+int vf_rotary_append(const vf_rotary_args *args, const void *q_dev, const void *k_dev, const void *v_dev,
+                     const float *table_dev, const int32_t *pos_dev, const int32_t *slot_dev, void *q_out_dev,
+                     void *kv_layer_dev, void *stream);
+
+typedef struct {
+    int32_t dtype, n_q_heads, n_kv_heads, head_dim;
+    int32_t n_seqs, total_rows;
+    int32_t max_rows, max_keys;    /* host's bounds of rows and of kv_len of a sequence: they choose kernels and */
+                                   /* the split of long contexts, results stand also where they are passed       */
+    int32_t pool_pages, max_pages, table_stride;
+    float scale;                   /* of the scores; 0: 1 / sqrt(head_dim)                    */
+    int64_t q_stride, out_stride;  /* elements between rows; multiples of 16 bytes            */
+} vf_packed_args;
+
+/* Bytes of workspace for these arguments (0: none needed).  (size_t)-1 on arguments the call refuses (see vf_last_error). */
+size_t vf_attention_packed_workspace(const vf_packed_args *args);
+
+/* Causal attention of packed rows with grouped heads.  Row i of sequence b stands at position
+ * p = kv_len[b] - rows_b + i and sees the keys 0 .. p of its pages:
+ *   out[row][h] = sum_t softmax_t(scale * q[row][h] . K[t][h / group]) V[t][h / group]
+ * Whole prompts (rows_b = kv_len[b]), chunks behind a cached prefix, drafts and single tokens may be mixed.
+ * A row that sees no key (p < 0, or kv_len 0 for a refused sequence) gets zeros; a page id outside the pool
+ * stands for 64 keys that are not there.  Keys that a row does not see add nothing to it, whatever memory
+ * holds there (also where it is not finite).  Rows outside row_off[0] .. row_off[n_seqs] are not written.
+ * bfloat16: scores, softmax and sums are float32, probabilities are rounded to bfloat16 for the product
+ * with V (to two bfloat16 values where few rows make that free).  Float32: float32 throughout. */
+int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const void *kv_layer_dev,
+                        const int32_t *block_table_dev, const int32_t *row_off_dev,
+                        const int32_t *kv_len_dev, void *out_dev, void *workspace_dev,
+                        size_t workspace_bytes, void *stream);
+
 /* ---- options ---------------------------------------------------------------------------------- */
 
 /* VF_OPT_FAST_PATH (default 1): vf_verify on a bfloat16 model with at most 48 rows in total runs

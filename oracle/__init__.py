@@ -35,8 +35,10 @@ from .reuse import reuse_segment, ReusePool
 from .tree import verify_tree, tree_greedy_accept, tree_stochastic_accept, compact
 from .calibration import topk_rows
 from .drafter import suffix_match_draft
+from . import packed
 
 __all__ = [
+    "packed",
     "round_bf16", "ModelSpec", "Weights", "KVCache", "forward", "prefill",
     "verify", "greedy_accept", "stochastic_accept", "first_token", "reuse_segment", "ReusePool",
     "verify_tree", "tree_greedy_accept", "tree_stochastic_accept", "compact", "topk_rows", "suffix_match_draft",

@@ -22,6 +22,9 @@ VF_TOPK_MAX = 8
 VF_ACCEPT_STATIC_MAX_ROWS = 512
 VF_OPT_FAST_PATH = 1
 VF_OPT_PERSISTENT = 2
+VF_PACKED_MAX_SEQS, VF_PACKED_MAX_ROWS = 4096, 1 << 20
+VF_ROTARY_HALF, VF_ROTARY_INTERLEAVED = 0, 1
+VF_ROTARY_UNSCALED, VF_ROTARY_POSITIONS, VF_ROTARY_BASE, VF_ROTARY_RAMP = 0, 1, 2, 3
 
 EXPORTS = [
     "vf_last_error", "vf_model_packed_bytes", "vf_model_create", "vf_model_destroy",
@@ -30,6 +33,7 @@ EXPORTS = [
     "vf_accept", "vf_accept_static", "vf_profile", "vf_profile_read", "vf_set_option", "vf_stream_read",
     "vf_reuse_select", "vf_reuse_pool_init", "vf_reuse_pool_update", "vf_reuse_pool_extend",
     "vf_verify_tree", "vf_accept_tree", "vf_prefill_chunk_topk", "vf_draft_suffix_match",
+    "vf_pages_assign", "vf_rotary_table", "vf_rotary_append", "vf_attention_packed_workspace", "vf_attention_packed",
 ]
 SITES = ["qkv", "o", "gateup", "down", "head", "attn", "small", "accept", "step"]
 
@@ -65,6 +69,23 @@ class vf_accept_params(C.Structure):
 class vf_reuse_pool(C.Structure):
     _fields_ = [("tokens", C.c_int32 * VF_MAX_DRAFTS)] + \
                [(n, C.c_int32) for n in ("len", "age", "max_age", "cap")]
+
+
+class vf_rotary_plan(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rotary_dim", "max_positions", "scaling", "pad")] + \
+               [(n, C.c_double) for n in ("theta", "factor", "low", "high", "trained", "magnitude")]
+
+
+class vf_rotary_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "pairs",
+                                         "total_rows", "max_positions", "pool_pages", "pad")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
+
+
+class vf_packed_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "n_seqs", "total_rows",
+                                         "max_rows", "max_keys", "pool_pages", "max_pages", "table_stride")] + \
+               [("scale", C.c_float)] + [(n, C.c_int64) for n in ("q_stride", "out_stride")]
 
 
 def _load():
@@ -106,6 +127,11 @@ def _load():
         "vf_reuse_pool_init": (C.c_int, [C.POINTER(vf_reuse_pool), C.c_int, C.c_int]),
         "vf_reuse_pool_update": (C.c_int, [C.POINTER(vf_reuse_pool), C.POINTER(i32), C.c_int, C.c_int, C.c_int]),
         "vf_reuse_pool_extend": (C.c_int, [C.POINTER(vf_reuse_pool), C.POINTER(i32), C.c_int]),
+        "vf_pages_assign": (C.c_int, [C.c_int] * 5 + [vp] * 11),
+        "vf_rotary_table": (C.c_int, [C.POINTER(vf_rotary_plan), vp, vp]),
+        "vf_rotary_append": (C.c_int, [C.POINTER(vf_rotary_args)] + [vp] * 9),
+        "vf_attention_packed_workspace": (sz, [C.POINTER(vf_packed_args)]),
+        "vf_attention_packed": (C.c_int, [C.POINTER(vf_packed_args)] + [vp] * 7 + [sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -372,3 +398,113 @@ def vf_stream_read(model):
 
 def vf_set_option(model, option, value):
     _check(lib.vf_set_option(model.handle, option, int(value)))
+
+
+# ---- packed batches ----------------------------------------------------------------------------
+
+def _refuse(what):
+    raise VfError(VF_ERR_ARG, what)
+
+
+def _ints(name, t, n):
+    """The address of an int32 device tensor of at least n entries one behind the other."""
+    if t.dtype != torch.int32 or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+        _refuse(f"{name}: contiguous int32 device tensor of {n} entries")
+    return t.data_ptr()
+
+
+def _rows(name, t, dtype, rows, heads, hd):
+    """The row stride of a device tensor [rows, heads, hd] whose rows are contiguous."""
+    if t.dtype != dtype or t.shape != (rows, heads, hd) or not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd):
+        _refuse(f"{name}: device tensor [{rows}, {heads}, {hd}] of {dtype} with contiguous rows")
+    return t.stride(0) if rows > 1 else max(t.stride(0), heads * hd)
+
+
+def _pool(t, hd, dtype):
+    """(pages, kv heads) of one layer's pages, [pages, 2, kv heads, 64 * hd]."""
+    if t.dim() != 4 or t.shape[1] != 2 or t.shape[3] != 64 * hd or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        _refuse(f"pool: contiguous device tensor [pages, 2, kv heads, {64 * hd}] of {dtype}")
+    return t.shape[0], t.shape[2]
+
+
+def _table(t):
+    """(sequences, entries a sequence, stride) of a block table."""
+    if t.dim() != 2 or t.dtype != torch.int32 or t.stride(1) != 1 or not t.is_cuda:
+        _refuse("block table: int32 device tensor [sequences, pages]")
+    n, m = t.shape
+    return n, m, t.stride(0) if n > 1 else max(t.stride(0), m)
+
+
+_DTYPES = {torch.bfloat16: VF_BF16, torch.float32: VF_F32}
+
+
+def _dtype(t):
+    return _DTYPES[t.dtype] if t.dtype in _DTYPES else _refuse(f"dtype {t.dtype}")
+
+
+def kv_layer(model, pool, layer):
+    """One layer of a pool of vf_kv_bytes(model, 64, n) bytes as the packed operators take it: a view
+    [n, 2, n_kv_heads, 64 * head_dim] in the model's type."""
+    c = model.cfg
+    t = pool.view(torch.bfloat16 if c.dtype == VF_BF16 else torch.float32)
+    return t.view(c.n_layers, -1, 2, c.n_kv_heads, 64 * c.head_dim)[layer]
+
+
+def vf_pages_assign(lens, new, free_pages, n_free, block_table, row_off, pos, slot, kv_len, n_free_out):
+    """int32 device tensors: lens, new [n], free_pages [any], n_free [1], block_table [n, pages]; results row_off [n + 1],
+    pos, slot [total rows], kv_len [n], n_free_out [1], and the fresh entries of block_table."""
+    n, m, stride = _table(block_table)
+    rows = pos.numel()
+    _check(lib.vf_pages_assign(n, m, stride, rows, free_pages.numel(), _ints("lens", lens, n), _ints("new", new, n),
+                               _ints("free_pages", free_pages, 0), _ints("n_free", n_free, 1), block_table.data_ptr(),
+                               _ints("row_off", row_off, n + 1), _ints("pos", pos, rows), _ints("slot", slot, rows),
+                               _ints("kv_len", kv_len, n), _ints("n_free_out", n_free_out, 1), _stream()))
+
+
+def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED, factor=1.0, low=0.0, high=0.0, trained=0.0,
+                    magnitude=1.0, device="cuda:0"):
+    """float32 [max_positions, rotary_dim / 2, 2]: cos and sin of every position's angles."""
+    plan = vf_rotary_plan(int(rotary_dim), int(max_positions), int(scaling), 0, theta, factor, low, high, trained, magnitude)
+    table = torch.empty((max(int(max_positions), 0), max(int(rotary_dim), 0) // 2, 2), dtype=torch.float32, device=device)
+    _check(lib.vf_rotary_table(C.byref(plan), _ptr(table), _stream()))
+    return table
+
+
+def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HALF):
+    """q, q_out [rows, q heads, hd], k, v [rows, kv heads, hd] (views of wider rows allowed), table of vf_rotary_table, pos and
+    slot int32 [rows], pool: one layer's pages (kv_layer)."""
+    rows, hq, hd = q.shape
+    pages, hkv = _pool(pool, hd, q.dtype)
+    if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous() or not table.is_cuda:
+        _refuse("table: contiguous float32 device tensor [positions, rotary_dim / 2, 2]")
+    args = vf_rotary_args(_dtype(q), hq, hkv, hd, 2 * table.shape[1], pairs, rows, table.shape[0], pages, 0,
+                          _rows("q", q, q.dtype, rows, hq, hd), _rows("k", k, q.dtype, rows, hkv, hd),
+                          _rows("v", v, q.dtype, rows, hkv, hd), _rows("q_out", q_out, q.dtype, rows, hq, hd))
+    _check(lib.vf_rotary_append(C.byref(args), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                                _ints("pos", pos, rows), _ints("slot", slot, rows), q_out.data_ptr(), pool.data_ptr(), _stream()))
+
+
+def _packed_args(q, pool, block_table, out, max_rows, max_keys, scale):
+    rows, hq, hd = q.shape
+    pages, hkv = _pool(pool, hd, q.dtype)
+    n, m, stride = _table(block_table)
+    q_stride = _rows("q", q, q.dtype, rows, hq, hd)
+    return vf_packed_args(_dtype(q), hq, hkv, hd, n, rows, max_rows, max_keys, pages, m, stride, scale, q_stride,
+                          q_stride if out is None else _rows("out", out, q.dtype, rows, hq, hd))
+
+
+def vf_attention_packed_workspace(q, pool, block_table, max_rows, max_keys):
+    """A workspace for vf_attention_packed with these arguments: uint8 device tensor."""
+    n = lib.vf_attention_packed_workspace(C.byref(_packed_args(q, pool, block_table, None, max_rows, max_keys, 0.0)))
+    if n == C.c_size_t(-1).value:
+        raise VfError(VF_ERR_ARG, lib.vf_last_error().decode())
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, max_keys, workspace, scale=0.0):
+    """q, out [rows, q heads, hd]; pool: one layer's pages; block_table int32 [n, pages]; row_off int32 [n + 1] and kv_len
+    int32 [n] on the device; max_rows, max_keys: the host's bounds of a sequence's rows and keys."""
+    args = _packed_args(q, pool, block_table, out, max_rows, max_keys, scale)
+    _check(lib.vf_attention_packed(C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
+                                   _ints("row_off", row_off, args.n_seqs + 1), _ints("kv_len", kv_len, args.n_seqs),
+                                   out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))

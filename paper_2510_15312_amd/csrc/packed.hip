@@ -1,0 +1,303 @@
+// A packed batch over the page pool: pages and slots for the tokens of a step, rotary embedding with the write to
+// the cache.  (Attention: packed_attention.hip.)
+#include <algorithm>
+#include <cmath>
+
+#include "vf_internal.h"
+
+namespace {
+
+// ---- pages -----------------------------------------------------------------------------------------
+
+constexpr int ASSIGN_THREADS = 256, ASSIGN_ROWS = 4;   // rows a thread
+
+struct AssignArgs {
+    int32_t n_seqs, max_pages, table_stride, total_rows, free_entries;
+    const int32_t *len, *add, *free_pages, *n_free;
+    int32_t *table, *row_off, *pos, *slot, *kv_len, *n_free_out;
+};
+
+__device__ __forceinline__ int pages_of(long long tokens) { return (int)((tokens + VF_TILE - 1) / VF_TILE); }
+
+// Largest i in [0, n) with v[i] <= x, for rising v with v[0] <= x.
+__device__ __forceinline__ int last_not_above(const int *v, int n, int x) {
+    int lo = 0;
+    for (int hi = n; hi - lo > 1;) {
+        const int mid = (lo + hi) >> 1;
+        if (v[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// need_b pages of sequence b come off the free list behind those of the sequences before it: two prefix sums over the
+// sequences (rows, pages) say where everything goes.  Every workgroup takes them for itself (at most 32 KB, from the caches)
+// and then its share of the rows and of the fresh table entries, so there is one launch and nobody waits for anybody.
+__global__ __launch_bounds__(ASSIGN_THREADS) void pages_assign_kernel(AssignArgs a) {
+    extern __shared__ int lds[];
+    int *off = lds, *before = lds + a.n_seqs + 1;           // rows, pages of the sequences before; pages: n_seqs + 1 entries
+    __shared__ long long wave_sum[2][ASSIGN_THREADS / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_seqs;
+    const int n_free = min(max(a.n_free[0], 0), a.free_entries);
+    long long rows = 0, pages = 0;                          // sums so far
+    for (int b0 = 0; b0 < n; b0 += ASSIGN_THREADS) {
+        const int b = b0 + tid;
+        const int h = b < n ? a.len[b] : 0, w = b < n ? a.add[b] : 0;
+        const long long end = (long long)h + w;
+        const bool fits = h >= 0 && w >= 0 && end <= (long long)a.max_pages * VF_TILE;
+        const int need = fits ? pages_of(end) - pages_of(h) : 0;
+        long long r = max(w, 0), p = need;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long r2 = __shfl_up(r, d, 64), p2 = __shfl_up(p, d, 64);
+            if (lane >= d) { r += r2; p += p2; }
+        }
+        if (lane == 63) { wave_sum[0][wave] = r; wave_sum[1][wave] = p; }
+        __syncthreads();
+        long long all_r = 0, all_p = 0;
+        for (int i = 0; i < ASSIGN_THREADS / 64; ++i) {
+            if (i < wave) { r += wave_sum[0][i]; p += wave_sum[1][i]; }
+            all_r += wave_sum[0][i];
+            all_p += wave_sum[1][i];
+        }
+        r += rows;
+        p += pages;
+        rows += all_r;
+        pages += all_p;
+        __syncthreads();
+        if (b < n) {
+            const bool granted = fits && (need == 0 || p <= n_free);
+            off[b + 1] = (int)min(r, (long long)a.total_rows);
+            // pages of the granted sequences: the sums stop rising at the first that is refused for want of pages, and
+            // from then on only sequences that need none are granted
+            before[b + 1] = (int)min(p, (long long)0x7fffffff);
+            if (blockIdx.x == 0) {
+                a.row_off[b + 1] = (int)min(r, (long long)a.total_rows);
+                a.kv_len[b] = granted ? (int)end : 0;
+            }
+        }
+    }
+    if (tid == 0) { off[0] = 0; before[0] = 0; }
+    __syncthreads();
+    // pages taken: the largest sum that the free list covers
+    const int used = before[last_not_above(before, n + 1, n_free)];
+    if (blockIdx.x == 0 && tid == 0) {
+        a.row_off[0] = 0;
+        a.n_free_out[0] = n_free - used;
+    }
+    const int step = gridDim.x * ASSIGN_THREADS, first = blockIdx.x * ASSIGN_THREADS + tid;
+    for (int e = first; e < used; e += step) {
+        const int b = last_not_above(before, n + 1, e);     // the last sequence that starts at or before e: it has pages
+        a.table[(size_t)b * a.table_stride + pages_of(a.len[b]) + (e - before[b])] = a.free_pages[n_free - 1 - e];
+    }
+    for (int r0 = first * ASSIGN_ROWS; r0 < a.total_rows; r0 += step * ASSIGN_ROWS) {
+        int b = last_not_above(off, n + 1, r0);
+        int h = 0, own = 0, next = 0;
+        bool granted = false, known = false;
+#pragma unroll
+        for (int i = 0; i < ASSIGN_ROWS; ++i) {
+            const int r = r0 + i;
+            if (r >= a.total_rows) break;
+            while (b < n && r >= off[b + 1]) { ++b; known = false; }
+            int pos = -1, slot = -1;
+            if (b < n) {
+                if (!known) {
+                    h = a.len[b];
+                    const int w = a.add[b];
+                    granted = h >= 0 && w >= 0 && (long long)h + w <= (long long)a.max_pages * VF_TILE &&
+                              (before[b + 1] == before[b] || before[b + 1] <= n_free);
+                    own = pages_of(max(h, 0));
+                    next = n_free - 1 - before[b];
+                    known = true;
+                }
+                if (granted) {
+                    pos = h + (r - off[b]);
+                    const int t = pos / VF_TILE;
+                    const int page = t < own ? a.table[(size_t)b * a.table_stride + t] : a.free_pages[next - (t - own)];
+                    slot = page < 0 || page > 0x7fffffff / VF_TILE - 1 ? -1 : page * VF_TILE + pos % VF_TILE;
+                }
+            }
+            a.pos[r] = pos;
+            a.slot[r] = slot;
+        }
+    }
+}
+
+// ---- rotary embedding and the write to the cache -------------------------------------------------
+
+__global__ void rotary_table_kernel(float2 *__restrict__ table, vf_rotary_plan p, int half) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= p.max_positions * half) return;
+    const int pos = i / half, j = i % half;
+    const double turn = 6.283185307179586476925;
+    double theta = p.theta;
+    if (p.scaling == VF_ROTARY_BASE) theta *= pow(p.factor, (double)p.rotary_dim / (p.rotary_dim - 2));
+    double f = pow(theta, -2.0 * j / p.rotary_dim);
+    if (p.scaling == VF_ROTARY_POSITIONS) f /= p.factor;
+    if (p.scaling == VF_ROTARY_RAMP) {
+        const double g = fmin(fmax((p.trained * f / turn - p.low) / (p.high - p.low), 0.0), 1.0);
+        f *= g + (1.0 - g) / p.factor;
+    }
+    double s, c;
+    sincos(pos * f, &s, &c);
+    table[i] = make_float2((float)(c * p.magnitude), (float)(s * p.magnitude));
+}
+
+template <typename T> struct alignas(16) Eight { T v[8]; };
+
+template <typename T> __device__ __forceinline__ Eight<T> eight(const T *p) { return *reinterpret_cast<const Eight<T> *>(p); }
+template <typename T> __device__ __forceinline__ void put_eight(T *p, const Eight<T> &x) { *reinterpret_cast<Eight<T> *>(p) = x; }
+
+// Sixteen elements of a head are a unit: eight pairs, which lie in two pieces of eight elements rotary_dim / 2 apart
+// (half) or next to one another (interleaved, and behind rotary_dim, where nothing turns).
+struct Unit { int lo, hi; bool turns; };
+__device__ __forceinline__ Unit unit_of(int u, int rotary_dim, bool half) {
+    const bool turns = u * 16 < rotary_dim;
+    if (half && turns) return {u * 8, rotary_dim / 2 + u * 8, true};
+    return {u * 16, u * 16 + 8, turns};
+}
+template <typename T> __device__ __forceinline__ void turn_unit(Eight<T> &lo, Eight<T> &hi, const float2 *angle, bool half) {
+    float x[16], y[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { x[i] = to_f32(lo.v[i]); x[8 + i] = to_f32(hi.v[i]); }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 a = angle[i];
+        const int p = half ? i : 2 * i, q = half ? 8 + i : 2 * i + 1;
+        y[p] = x[p] * a.x - x[q] * a.y;
+        y[q] = x[q] * a.x + x[p] * a.y;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo.v[i] = from_f32<T>(y[i]); hi.v[i] = from_f32<T>(y[8 + i]); }
+}
+
+// One thread: one unit of one head of a row of q or k, or eight elements of a row of v.
+template <typename T, int HD, bool HALF>
+__global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, const T *q, const T *__restrict__ k,
+                                                            const T *__restrict__ v, const float2 *__restrict__ table,
+                                                            const int32_t *__restrict__ pos, const int32_t *__restrict__ slot,
+                                                            T *q_out, T *__restrict__ kv) {
+    const int hq = a.n_q_heads, hkv = a.n_kv_heads, per_row = (hq + hkv) * (HD / 16) + hkv * (HD / 8);
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(id / per_row), i = (int)(id % per_row);
+    if (row >= a.total_rows) return;
+    const int p = pos[row], s = slot[row];
+    const bool at = p >= 0 && p < a.max_positions, stored = at && s >= 0 && s / VF_TILE < a.pool_pages;
+    const int page = s / VF_TILE, tin = s % VF_TILE;
+    if (i < (hq + hkv) * (HD / 16)) {
+        const int head = i / (HD / 16);
+        const Unit u = unit_of(i % (HD / 16), a.rotary_dim, HALF);
+        const bool is_q = head < hq;
+        if (!is_q && !stored) return;
+        const T *src = is_q ? q + row * a.q_stride + head * HD : k + row * a.k_stride + (head - hq) * HD;
+        Eight<T> lo = eight(src + u.lo), hi = eight(src + u.hi);
+        if (at && u.turns) turn_unit(lo, hi, table + (size_t)p * (a.rotary_dim / 2) + i % (HD / 16) * 8, HALF);
+        if (is_q) {
+            if (!at) lo = hi = Eight<T>{};
+            T *dst = q_out + row * a.q_out_stride + head * HD;
+            put_eight(dst + u.lo, lo);
+            put_eight(dst + u.hi, hi);
+        } else {
+            put_eight(kv + kv_k_index(0, 0, page, hkv, head - hq, tin, u.lo, HD), lo);
+            put_eight(kv + kv_k_index(0, 0, page, hkv, head - hq, tin, u.hi, HD), hi);
+        }
+    } else if (stored) {
+        const int j = i - (hq + hkv) * (HD / 16), head = j / (HD / 8), d0 = j % (HD / 8) * 8;
+        const Eight<T> x = eight(v + row * a.v_stride + head * HD + d0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) kv[kv_v_index(0, 0, page, hkv, head, tin, d0 + e, HD)] = x.v[e];
+    }
+}
+
+template <typename T, int HD>
+int launch_rotary(const vf_rotary_args &a, const void *q, const void *k, const void *v, const float *table, const int32_t *pos,
+                   const int32_t *slot, void *q_out, void *kv, hipStream_t st) {
+    const long long threads = (long long)a.total_rows * ((a.n_q_heads + a.n_kv_heads) * (HD / 16) + a.n_kv_heads * (HD / 8));
+    if (threads >= 0xffffff00LL) return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: %d rows of %d heads in one call", a.total_rows, a.n_q_heads + 2 * a.n_kv_heads);
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    if (a.pairs == VF_ROTARY_HALF)
+        hipLaunchKernelGGL((rotary_append_kernel<T, HD, true>), grid, dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v,
+                           (const float2 *)table, pos, slot, (T *)q_out, (T *)kv);
+    else
+        hipLaunchKernelGGL((rotary_append_kernel<T, HD, false>), grid, dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v,
+                           (const float2 *)table, pos, slot, (T *)q_out, (T *)kv);
+    VF_LAUNCH_CHECK("rotary_append");
+    return VF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int vf_pages_assign(int n_seqs, int max_pages, int table_stride, int total_rows, int free_entries, const int32_t *len_dev,
+                    const int32_t *new_dev, const int32_t *free_pages_dev, const int32_t *n_free_dev, int32_t *block_table_dev,
+                    int32_t *row_off_dev, int32_t *pos_dev, int32_t *slot_dev, int32_t *kv_len_dev, int32_t *n_free_out_dev,
+                    void *stream) {
+    if (n_seqs < 1 || n_seqs > VF_PACKED_MAX_SEQS) return vf_fail(VF_ERR_ARG, "vf_pages_assign: n_seqs %d (1 to %d)", n_seqs, VF_PACKED_MAX_SEQS);
+    if (max_pages < 1 || max_pages > 0x7fffffff / VF_TILE || table_stride < max_pages || total_rows < 0 || total_rows > VF_PACKED_MAX_ROWS ||
+        free_entries < 0 || free_entries > 0x7fffffff / VF_TILE)
+        return vf_fail(VF_ERR_ARG, "vf_pages_assign: max_pages %d, table_stride %d, total_rows %d, free_entries %d", max_pages,
+                       table_stride, total_rows, free_entries);
+    if (!len_dev || !new_dev || (!free_pages_dev && free_entries) || !n_free_dev || !block_table_dev || !row_off_dev ||
+        ((!pos_dev || !slot_dev) && total_rows) || !kv_len_dev || !n_free_out_dev)
+        return vf_fail(VF_ERR_ARG, "vf_pages_assign: NULL argument");
+    if (kv_len_dev == len_dev || kv_len_dev == new_dev || n_free_out_dev == n_free_dev)
+        return vf_fail(VF_ERR_ARG, "vf_pages_assign: an output is an input");
+    const AssignArgs a = {n_seqs, max_pages, table_stride, total_rows, free_entries, len_dev, new_dev, free_pages_dev, n_free_dev,
+                          block_table_dev, row_off_dev, pos_dev, slot_dev, kv_len_dev, n_free_out_dev};
+    const int blocks = std::max(1, std::min(256, (int)(((long long)total_rows + ASSIGN_THREADS * ASSIGN_ROWS - 1) / (ASSIGN_THREADS * ASSIGN_ROWS))));
+    hipLaunchKernelGGL(pages_assign_kernel, dim3(blocks), dim3(ASSIGN_THREADS), (size_t)(n_seqs + 1) * 2 * sizeof(int),
+                       (hipStream_t)stream, a);
+    VF_LAUNCH_CHECK("pages_assign");
+    return VF_OK;
+}
+
+int vf_rotary_table(const vf_rotary_plan *plan, float *table_dev, void *stream) {
+    if (!plan || !table_dev) return vf_fail(VF_ERR_ARG, "vf_rotary_table: NULL argument");
+    const vf_rotary_plan &p = *plan;
+    if (p.rotary_dim < 16 || p.rotary_dim > 128 || p.rotary_dim % 16 || p.max_positions < 1 || p.max_positions > (1 << 24))
+        return vf_fail(VF_ERR_ARG, "vf_rotary_table: rotary_dim %d, max_positions %d", p.rotary_dim, p.max_positions);
+    if (!(p.theta > 0) || !std::isfinite(p.theta) || !std::isfinite(p.magnitude)) return vf_fail(VF_ERR_ARG, "vf_rotary_table: theta %g, magnitude %g", p.theta, p.magnitude);
+    if (p.scaling < VF_ROTARY_UNSCALED || p.scaling > VF_ROTARY_RAMP) return vf_fail(VF_ERR_ARG, "vf_rotary_table: scaling %d", p.scaling);
+    if (p.scaling != VF_ROTARY_UNSCALED && (!(p.factor > 0) || !std::isfinite(p.factor))) return vf_fail(VF_ERR_ARG, "vf_rotary_table: factor %g", p.factor);
+    if (p.scaling == VF_ROTARY_RAMP && (!(p.trained > 0) || !std::isfinite(p.trained) || !(p.high > p.low) || !std::isfinite(p.high) || !std::isfinite(p.low)))
+        return vf_fail(VF_ERR_ARG, "vf_rotary_table: ramp from %g to %g turns over %g positions", p.low, p.high, p.trained);
+    const int half = p.rotary_dim / 2;
+    const long long n = (long long)p.max_positions * half;
+    hipLaunchKernelGGL(rotary_table_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, (hipStream_t)stream, (float2 *)table_dev, p, half);
+    VF_LAUNCH_CHECK("rotary_table");
+    return VF_OK;
+}
+
+int vf_rotary_append(const vf_rotary_args *args, const void *q_dev, const void *k_dev, const void *v_dev, const float *table_dev,
+                     const int32_t *pos_dev, const int32_t *slot_dev, void *q_out_dev, void *kv_layer_dev, void *stream) {
+    if (!args) return vf_fail(VF_ERR_ARG, "vf_rotary_append: NULL argument");
+    const vf_rotary_args &a = *args;
+    if (a.dtype != VF_F32 && a.dtype != VF_BF16) return vf_fail(VF_ERR_ARG, "vf_rotary_append: dtype %d", a.dtype);
+    if (a.n_q_heads < 1 || a.n_kv_heads < 1 || a.n_q_heads > 256 || a.n_kv_heads > 256)
+        return vf_fail(VF_ERR_ARG, "vf_rotary_append: %d query heads, %d key heads", a.n_q_heads, a.n_kv_heads);
+    if (a.head_dim != 64 && a.head_dim != 128) return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: head_dim %d (built for 64 and 128)", a.head_dim);
+    if (a.rotary_dim < 16 || a.rotary_dim > a.head_dim || a.rotary_dim % 16)
+        return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: rotary_dim %d of head_dim %d (multiples of 16)", a.rotary_dim, a.head_dim);
+    if (a.pairs != VF_ROTARY_HALF && a.pairs != VF_ROTARY_INTERLEAVED) return vf_fail(VF_ERR_ARG, "vf_rotary_append: pairs %d", a.pairs);
+    if (a.total_rows < 0 || a.total_rows > VF_PACKED_MAX_ROWS || a.max_positions < 1 || a.pool_pages < 1 || a.pool_pages > 0x7fffffff / VF_TILE)
+        return vf_fail(VF_ERR_ARG, "vf_rotary_append: %d rows, %d positions, %d pages", a.total_rows, a.max_positions, a.pool_pages);
+    if (a.total_rows == 0) return VF_OK;
+    if (!q_dev || !k_dev || !v_dev || !table_dev || !pos_dev || !slot_dev || !q_out_dev || !kv_layer_dev)
+        return vf_fail(VF_ERR_ARG, "vf_rotary_append: NULL argument");
+    const int es = a.dtype == VF_BF16 ? 2 : 4;
+    const int64_t wq = (int64_t)a.n_q_heads * a.head_dim, wkv = (int64_t)a.n_kv_heads * a.head_dim;
+    if (a.q_stride < wq || a.q_out_stride < wq || a.k_stride < wkv || a.v_stride < wkv)
+        return vf_fail(VF_ERR_ARG, "vf_rotary_append: rows overlap (strides %lld, %lld, %lld, %lld)", (long long)a.q_stride,
+                       (long long)a.k_stride, (long long)a.v_stride, (long long)a.q_out_stride);
+    if (q_out_dev == q_dev && a.q_out_stride != a.q_stride) return vf_fail(VF_ERR_ARG, "vf_rotary_append: q in place with another stride");
+    if (((a.q_stride | a.k_stride | a.v_stride | a.q_out_stride) * es | (int64_t)(uintptr_t)q_dev | (int64_t)(uintptr_t)k_dev |
+         (int64_t)(uintptr_t)v_dev | (int64_t)(uintptr_t)q_out_dev | (int64_t)(uintptr_t)kv_layer_dev) & 15 || (uintptr_t)table_dev & 7)
+        return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: addresses and strides are multiples of 16 bytes");
+    hipStream_t st = (hipStream_t)stream;
+    const auto launch = a.dtype == VF_BF16 ? (a.head_dim == 128 ? launch_rotary<bf16_t, 128> : launch_rotary<bf16_t, 64>)
+                                           : (a.head_dim == 128 ? launch_rotary<float, 128> : launch_rotary<float, 64>);
+    return launch(a, q_dev, k_dev, v_dev, table_dev, pos_dev, slot_dev, q_out_dev, kv_layer_dev, st);
+}
+
+}  // extern "C"

@@ -415,7 +415,7 @@ typedef struct {
     int32_t max_rows, max_keys;    /* host's bounds of rows and of kv_len of a sequence: they choose kernels and */
                                    /* the split of long contexts, results stand also where they are passed       */
     int32_t pool_pages, max_pages, table_stride;
-    float scale;                   /* of the scores; 0: 1 / sqrt(head_dim)                    */
+    float scale;                   /* of the scores, not negative; 0: 1 / sqrt(head_dim)      */
     int64_t q_stride, out_stride;  /* elements between rows; multiples of 16 bytes            */
 } vf_packed_args;
 

@@ -143,8 +143,6 @@ __global__ void rotary_table_kernel(float2 *__restrict__ table, vf_rotary_plan p
     table[i] = make_float2((float)(c * p.magnitude), (float)(s * p.magnitude));
 }
 
-template <typename T> struct alignas(16) Eight { T v[8]; };
-
 template <typename T> __device__ __forceinline__ Eight<T> eight(const T *p) { return *reinterpret_cast<const Eight<T> *>(p); }
 template <typename T> __device__ __forceinline__ void put_eight(T *p, const Eight<T> &x) { *reinterpret_cast<Eight<T> *>(p) = x; }
 

@@ -1,8 +1,15 @@
 // Causal attention of packed rows with grouped heads over the page pool: whole prompts, chunks behind a cached prefix,
 // drafts and single tokens of many sequences in one call.
+//
+// The rows of a sequence and the query heads of one key head are its items, row-major: all items of a key head meet the same
+// keys, so a tile of items reads them once whatever the group is, and few rows fill a tile as well as they can.
+// With S = K Q^T (keys down, items across) a lane holds one item's scores, so the softmax is arithmetic inside a lane and one
+// exchange between the wavefront's halves, and S is already the operand of O^T = V^T P^T.
 #include <algorithm>
 #include <cmath>
 
+#include "fast_common.h"
+#include "lds_stream.h"
 #include "vf_internal.h"
 
 namespace {
@@ -12,48 +19,320 @@ struct PackedAttn {
     const void *q, *kv;
     const int32_t *table, *row_off, *kv_len;
     void *out;
+    int32_t group, tiles, parts, part_pages;   // tiles: items tiles of all sequences, at most
+    float scale_log2e;
+    float *records;                            // [row][head][part][REC_HEAD + head_dim], parts > 1
+    int32_t *used;                             // [row]: parts with a record
 };
+constexpr int REC_HEAD = 4;                    // maximum, sum, -, -
 
-// One wavefront per row and query head: a key per lane for the scores, HD / 64 elements per lane for the sums.
-template <typename T, int HD>
-__global__ __launch_bounds__(64) void attention_plain_kernel(PackedAttn p) {
-    const vf_packed_args &a = p.a;
-    __shared__ float qs[HD];
-    const int row = blockIdx.x, head = blockIdx.y, lane = threadIdx.x, kvh = head / (a.n_q_heads / a.n_kv_heads);
-    int b = 0;
-    while (b < a.n_seqs && row >= p.row_off[b + 1]) ++b;
-    if (b == a.n_seqs || row < p.row_off[b]) return;
-    const int rows = min(p.row_off[b + 1], a.total_rows) - p.row_off[b];
-    const int last = min(p.kv_len[b] - rows + row - p.row_off[b], min(p.kv_len[b], a.max_pages * VF_TILE) - 1);
-    const T *q = (const T *)p.q + row * a.q_stride + head * HD, *kv = (const T *)p.kv;
-    for (int d = lane; d < HD; d += 64) qs[d] = to_f32(q[d]);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, acc[HD / 64] = {};
-    for (int t0 = 0; t0 <= last; t0 += VF_TILE) {
-        const int page = p.table[(size_t)b * a.table_stride + t0 / VF_TILE];
-        if (page < 0 || page >= a.pool_pages) continue;
-        float s = -INFINITY;
-        if (t0 + lane <= last) {
-            s = 0.f;
-            for (int d = 0; d < HD; ++d) s += qs[d] * to_f32(kv[kv_k_index(0, 0, page, a.n_kv_heads, kvh, lane, d, HD)]);
-            s *= a.scale;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// A tile of BM items: its sequence's rows and keys.  rows <= 0: none.
+struct Tile { int seq, item0, row0, rows, kv_len; };
+__device__ __forceinline__ int2 seq_rows(const PackedAttn &p, int b) {   // first row and rows, whatever the offsets hold
+    const int r0 = min(max(p.row_off[b], 0), p.a.total_rows), r1 = min(max(p.row_off[b + 1], r0), p.a.total_rows);
+    return {r0, r1 - r0};
+}
+// Tiles are counted sequence by sequence, 64 sequences at a time.
+template <int BM> __device__ __forceinline__ Tile find_tile(const PackedAttn &p, int tile) {
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0, base = 0; b0 < p.a.n_seqs; b0 += 64) {
+        const int b = min(b0 + lane, p.a.n_seqs - 1);
+        const int2 r = seq_rows(p, b);
+        const int len = p.kv_len[b];
+        int upto = b0 + lane < p.a.n_seqs ? (int)(((long long)r.y * p.group + BM - 1) / BM) : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += x;
         }
-        float mx = s;
-        for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-        const float m_new = fmaxf(m, mx), keep = m == -INFINITY ? 0.f : expf(m - m_new);
-        float w = t0 + lane <= last ? expf(s - m_new) : 0.f;
-        l = l * keep + w;
-        for (int i = 0; i < HD / 64; ++i) acc[i] *= keep;
-        m = m_new;
-        for (int j = 0; j <= min(VF_TILE - 1, last - t0); ++j) {
-            const float wj = __shfl(w, j, 64);
-            for (int i = 0; i < HD / 64; ++i)
-                acc[i] += wj * to_f32(kv[kv_v_index(0, 0, page, a.n_kv_heads, kvh, j, lane + 64 * i, HD)]);
+        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(base + upto > tile);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond);
+            const int before = base + (at ? __builtin_amdgcn_readlane(upto, at - 1) : 0);
+            return {b0 + at, (tile - before) * BM, __builtin_amdgcn_readlane(r.x, at), __builtin_amdgcn_readlane(r.y, at),
+                    __builtin_amdgcn_readlane(len, at)};
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {0, 0, 0, 0, 0};
+}
+
+__device__ __forceinline__ float halves_max(float x) {
+    float y = x;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return fmaxf(x, y);
+}
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+
+// Operands of a 32x32 product over 16 values of k (32 lanes each take 8): bfloat16 in one matrix instruction, float32 in eight.
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> { bf16x8 v; };
+template <> struct Frag<float> { float v[8]; };
+__device__ __forceinline__ floatx16 mma(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mma(const Frag<float> &a, const Frag<float> &b, floatx16 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
+template <typename T> __device__ __forceinline__ bool any_not_finite(const Frag<T> &f) {
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bad |= not_finite(to_f32(f.v[j]));
+    return bad;
+}
+
+// Tiles of 32 items a wavefront, pages of 64 keys through LDS.
+//
+// A page comes as direct loads of 1 KB units, S - 1 pages ahead.  Units hold 16 bytes a lane: a K or V piece of eight elements
+// in bfloat16, half of one in float32 (the halves of a fragment's pieces in two units, so that a read of 16 bytes a lane
+// touches every bank once).  K rows are taken in the order that leaves a lane with eight consecutive keys per operand of
+// the second product: row m of a 32-key tile is key 16 (m >> 4) + 8 (m >> 2 & 1) + 4 (m >> 3 & 1) + (m & 3).
+template <typename T, int HD, int WAVES, int S>
+__global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAttn p) {
+    constexpr int BM = WAVES * 32, HALVES = sizeof(T) / 2, UNITS = HD / 4 * HALVES, LPW = UNITS / WAVES;   // units of a page
+    constexpr int KD = HD / 32, KS = HD / 16, DB = HD / 32;
+    static_assert(UNITS % (2 * WAVES) == 0, "a wavefront loads K or V");
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const vf_packed_args &a = p.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int part = rest % p.parts;
+    const Tile t = find_tile<BM>(p, p.tiles - 1 - rest / p.parts);
+    if (t.rows <= 0) return;
+    const int group = p.group, n_items = t.rows * group, cap = min(t.kv_len, a.max_pages * VF_TILE);
+    const int first_pos = t.kv_len - t.rows;                    // position of row 0
+    const int wave0 = t.item0 + wave * 32, item = min(n_items - 1, wave0 + col);
+    const int row = t.row0 + item / group, head = kvh * group + item % group;
+    const int last_key = min(first_pos + item / group, cap - 1);
+    const int tile_last = min(first_pos + min(n_items - 1, t.item0 + BM - 1) / group, cap - 1);
+    const int wave_last = wave0 < n_items ? min(first_pos + min(n_items - 1, wave0 + 31) / group, cap - 1) : -1;
+    const int wave_first = min(first_pos + min(n_items - 1, wave0) / group, cap - 1);
+    const int pages = tile_last < 0 ? 0 : tile_last / VF_TILE + 1;
+    const int p_begin = part * p.part_pages, p_end = part == p.parts - 1 ? pages : min(pages, p_begin + p.part_pages);
+    if (p.parts > 1 && part == 0 && kvh == 0 && wave0 + col < n_items && half == 0 && item % group == 0)
+        p.used[row] = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
+    if (p_begin >= p_end && part > 0) return;
+
+    Frag<T> qf[KS];
+    {
+        const T *q = (const T *)p.q + row * a.q_stride + head * HD + half * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const Eight<T> x = *reinterpret_cast<const Eight<T> *>(q + s * 16);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) qf[s].v[j] = x.v[j];
         }
     }
-    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d, 64);
-    for (int i = 0; i < HD / 64; ++i)
-        ((T *)p.out)[row * a.out_stride + head * HD + lane + 64 * i] = from_f32<T>(m == -INFINITY ? 0.f : acc[i] / l);
+    const size_t page_bytes = (size_t)2 * a.n_kv_heads * VF_TILE * HD * sizeof(T);
+    const char *src = (const char *)p.kv + (size_t)(wave < WAVES / 2 ? kvh : a.n_kv_heads + kvh) * (VF_TILE * HD * sizeof(T)) +
+                      wave % (WAVES / 2) * (LPW * 1024);
+    const unsigned lds0 = lds_address(smem) + wave * (LPW * 1024);
+    const int32_t *table = p.table + (size_t)t.seq * a.table_stride;
+    // ids of 64 pages, one per lane: those from `at` on
+    int ids = 0, ids_at = -64;
+    auto page_id = [&](int pg) {
+        if (pg - ids_at >= 64) {
+            ids_at = pg;
+            ids = table[min(pg + lane, a.max_pages - 1)];
+        }
+        const int id = __builtin_amdgcn_readlane(ids, pg - ids_at);
+        return (unsigned)id < (unsigned)a.pool_pages ? id : -1;
+    };
+    unsigned long long there = 0;   // bit i: page i (mod 64) of the ring is in the pool
+    auto issue = [&](int i) {
+        const int pg = p_begin + i;
+        if (pg >= p_end) {   // nothing to load; the count of loads in flight stays what the waits assume
+            static_for<0, LPW>([&](auto f) { fragment_to_lds<(int)f * 1024>(src, lane * 16, lds0 + (unsigned)i % S * (UNITS * 1024)); });
+            return;
+        }
+        const int id = page_id(pg);
+        there = (there & ~(1ull << (i & 63))) | (unsigned long long)(id >= 0) << (i & 63);
+        const char *from = src + (size_t)max(id, 0) * page_bytes;
+        const unsigned dst = lds0 + (unsigned)i % S * (UNITS * 1024);
+        static_for<0, LPW>([&](auto f) {
+            constexpr int F = f;
+            if constexpr (HALVES == 1) fragment_to_lds<F * 1024>(from + F * 1024, lane * 16, dst);
+            else fragment_to_lds<F * 1024>(from + F / 2 * 2048 + F % 2 * 16, lane * 32, dst);
+        });
+    };
+    // a lane's pieces: K row col of a 32-key tile, V^T row col of 32 output dimensions
+    const unsigned k_lane = (unsigned)((col >> 3 & 1) * KD * 64 * HALVES + half * 16 + (col >> 4) * 8 + (col >> 2 & 1) * 4 + (col & 3)) * 16;
+    const unsigned v_lane = (unsigned)((col >> 4) * 64 * HALVES + half * 16 + (col & 15)) * 16;
+    auto piece = [&](const unsigned char *at) {
+        Frag<T> f;
+        if constexpr (HALVES == 1) f.v = *reinterpret_cast<const bf16x8 *>(at);
+        else
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const floatx4 x = *reinterpret_cast<const floatx4 *>(at + h * 1024);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f.v[h * 4 + j] = x[j];
+            }
+        return f;
+    };
+    auto k_piece = [&](const unsigned char *st, int kt, int s) { return piece(st + k_lane + (kt * 2 * KD + s / 2) * 1024 * HALVES + s % 2 * 512); };
+    auto v_piece = [&](const unsigned char *st, int kt, int tt, int db) {
+        return piece(st + UNITS / 2 * 1024 + v_lane + (kt * 2 * DB + db * 2) * 1024 * HALVES + tt * 512);
+    };
+    floatx16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+    float m_run = -1e30f, l_run = 0.f;   // l_run: this lane's keys
+    auto update = [&](const unsigned char *st, int t0, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        floatx16 sc[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[kt][i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) sc[kt] = mma(k_piece(st, kt, s), qf[s], sc[kt]);
+        const int own = t0 + half * 8;   // key of register i of tile kt: own + 32 kt + 16 (i >> 3) + (i & 7)
+        if constexpr (MASKED)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (own + kt * 32 + (i >> 3) * 16 + (i & 7) > last_key) sc[kt][i] = -INFINITY;
+        float mx = sc[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
+        mx = halves_max(mx) * p.scale_log2e;
+        // The weights' common factor follows the maximum with slack: they stay below 2^8, and the sums are rescaled in few pages.
+        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
+            const float m_new = fmaxf(m_run, mx), keep = __builtin_amdgcn_exp2f(m_run - m_new);
+            l_run *= keep;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= keep;
+            m_run = m_new;
+        }
+        Frag<T> w[4];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(sc[i >> 4][i & 15], p.scale_log2e, -m_run));
+            l_run += x;
+            w[i >> 3].v[i & 7] = from_f32<T>(x);
+        }
+        // O^T += V^T W^T of 32 output dimensions; MASKED: keys beyond `seen` are taken as zeros
+        auto product = [&](auto db, int seen, floatx16 c) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) {
+                    Frag<T> v = v_piece(st, kt, tt, db);
+                    if constexpr (MASKED)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (own + kt * 32 + tt * 16 + j > seen) v.v[j] = from_f32<T>(0.f);
+                    c = mma(v, w[kt * 2 + tt], c);
+                }
+            return c;
+        };
+        static_for<0, DB>([&](auto db) {
+            constexpr int D = db;
+            if constexpr (MASKED) {
+                // 0 times a value that is not finite is not 0: keys beyond all items count as zeros, and if a key that only some
+                // items see holds such a value, every row takes the product with its own keys
+                bool bad = false;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt) {
+                        const Frag<T> v = v_piece(st, kt, tt, D);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) bad |= own + kt * 32 + tt * 16 + j <= wave_last && not_finite(to_f32(v.v[j]));
+                    }
+                if (__builtin_amdgcn_ballot_w64(bad)) {
+                    floatx16 sum = acc[D];   // of rows that see nothing here
+                    for (int seen = max(wave_first, t0); seen <= min(wave_last, t0 + VF_TILE - 1); ++seen) {
+                        const floatx16 c = product(db, seen, acc[D]);
+                        if (min(last_key, t0 + VF_TILE - 1) == seen) sum = c;
+                    }
+                    acc[D] = sum;
+                    return;
+                }
+            }
+            acc[D] = product(db, wave_last, acc[D]);
+        });
+    };
+    const int n = p_end - p_begin;
+    if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i) issue(i);
+        for (int i = 0; i < n; ++i) {
+            vm_wait<(S - 2) * LPW>();   // page i has landed; behind the barrier everyone's share of it has,
+            lds_sync();                 // and page i - 1 has been read, so its slot takes page i + S - 1
+            issue(i + S - 1);
+            const int t0 = (p_begin + i) * VF_TILE;
+            const unsigned char *st = smem + (unsigned)i % S * (UNITS * 1024);
+            if (t0 > wave_last || !(there >> (i & 63) & 1)) continue;
+            if (t0 + VF_TILE - 1 <= wave_first) update(st, t0, std::false_type{});
+            else update(st, t0, std::true_type{});
+        }
+        vm_wait<0>();   // nothing is on its way to LDS when the workgroup ends
+    }
+    const float sum = l_run + __shfl_xor(l_run, 32, 64);
+    if (wave0 + col >= n_items) return;
+    // a lane's values: d = 32 db + 8 j + 4 half + r
+    if (p.parts > 1) {
+        float *rec = p.records + (((size_t)row * a.n_q_heads + head) * p.parts + part) * (REC_HEAD + HD);
+        if (half == 0) *reinterpret_cast<float2 *>(rec) = float2{m_run, sum};
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<floatx4 *>(rec + REC_HEAD + db * 32 + j * 8 + half * 4) =
+                    floatx4{acc[db][j * 4], acc[db][j * 4 + 1], acc[db][j * 4 + 2], acc[db][j * 4 + 3]};
+        return;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    T *out = (T *)p.out + row * a.out_stride + head * HD + half * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            typedef T four __attribute__((ext_vector_type(4)));
+            four x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = from_f32<T>(acc[db][j * 4 + r] * inv);
+            *reinterpret_cast<four *>(out + db * 32 + j * 8) = x;
+        }
+}
+
+// Merge of the parts: HD / 4 threads per row and head.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
+    constexpr int REC = HD + REC_HEAD, TH = HD / 4;
+    const vf_packed_args &a = p.a;
+    const long long idx = (long long)blockIdx.x * (256 / TH) + threadIdx.x / TH;
+    const int row = (int)(idx / a.n_q_heads), head = (int)(idx % a.n_q_heads), d0 = threadIdx.x % TH * 4;
+    if (row >= a.total_rows || row < p.row_off[0] || row >= p.row_off[a.n_seqs]) return;
+    const int used = p.used[row];
+    const float *rec = p.records + ((size_t)row * a.n_q_heads + head) * p.parts * REC;
+    float M = -1e30f, L = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < used; ++i, rec += REC) {
+        const float2 ml = *reinterpret_cast<const float2 *>(rec);
+        const floatx4 v = *reinterpret_cast<const floatx4 *>(rec + REC_HEAD + d0);
+        const float m = fmaxf(M, ml.x), keep = __builtin_amdgcn_exp2f(M - m), add = __builtin_amdgcn_exp2f(ml.x - m);
+        L = L * keep + ml.y * add;
+        acc = acc * keep + v * add;
+        M = m;
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    typedef T four __attribute__((ext_vector_type(4)));
+    four x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = from_f32<T>(acc[r] * inv);
+    *reinterpret_cast<four *>((T *)p.out + row * a.out_stride + head * HD + d0) = x;
 }
 
 int check(const char *name, const vf_packed_args *args) {
@@ -69,12 +348,49 @@ int check(const char *name, const vf_packed_args *args) {
         a.max_pages > 0x7fffffff / VF_TILE || a.table_stride < a.max_pages)
         return vf_fail(VF_ERR_ARG, "%s: max_rows %d, max_keys %d, pool_pages %d, max_pages %d, table_stride %d", name, a.max_rows,
                        a.max_keys, a.pool_pages, a.max_pages, a.table_stride);
-    if (!std::isfinite(a.scale)) return vf_fail(VF_ERR_ARG, "%s: scale %g", name, a.scale);
+    if (!std::isfinite(a.scale) || a.scale < 0) return vf_fail(VF_ERR_ARG, "%s: scale %g", name, a.scale);
     const int64_t w = (int64_t)a.n_q_heads * a.head_dim;
     if (a.q_stride < w || a.out_stride < w)
         return vf_fail(VF_ERR_ARG, "%s: rows overlap (strides %lld, %lld)", name, (long long)a.q_stride, (long long)a.out_stride);
     if ((a.q_stride | a.out_stride) * (a.dtype == VF_BF16 ? 2 : 4) & 15)
         return vf_fail(VF_ERR_UNSUPPORTED, "%s: strides are multiples of 16 bytes", name);
+    return VF_OK;
+}
+
+// Kernel, tiles and parts of a call, from what the host knows.
+struct Plan { int waves, tiles, parts, part_pages; size_t bytes; };
+
+Plan make_plan(const vf_packed_args &a) {
+    Plan r{};
+    const int group = a.n_q_heads / a.n_kv_heads;
+    r.waves = 4;
+    const int bm = r.waves * 32;
+    const long long items = (long long)a.total_rows * group;
+    r.tiles = (int)(items / bm + std::min(a.n_seqs, a.total_rows));   // a sequence ends in one tile that is not full
+    const int pages = std::max(1, std::min(a.max_pages, (a.max_keys + VF_TILE - 1) / VF_TILE));
+    const long long groups = (long long)std::max<long long>(1, std::min<long long>(r.tiles, (items + bm - 1) / bm)) * a.n_kv_heads;
+    r.parts = (int)std::max(1ll, std::min<long long>((512 + groups - 1) / groups, pages / 4));
+    r.part_pages = (pages + r.parts - 1) / r.parts;
+    r.parts = (pages + r.part_pages - 1) / r.part_pages;
+    if (r.parts > 1)
+        r.bytes = (size_t)a.total_rows * a.n_q_heads * r.parts * (REC_HEAD + a.head_dim) * sizeof(float) + (size_t)a.total_rows * sizeof(int32_t);
+    return r;
+}
+
+template <typename T, int HD>
+int launch(PackedAttn &p, const Plan &plan, hipStream_t st) {
+    constexpr int WAVES = 4, S = 2, LDS = S * HD / 4 * 1024 * (int)sizeof(T) / 2;
+    static const hipError_t set = hipFuncSetAttribute((const void *)attention_tiles_kernel<T, HD, WAVES, S>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    VF_HIP(set);
+    const long long blocks = (long long)plan.tiles * plan.parts * p.a.n_kv_heads;
+    if (blocks > 0x7fffff) return vf_fail(VF_ERR_UNSUPPORTED, "vf_attention_packed: %lld workgroups", blocks);
+    hipLaunchKernelGGL((attention_tiles_kernel<T, HD, WAVES, S>), dim3((unsigned)blocks), dim3(WAVES * 64), LDS, st, p);
+    VF_LAUNCH_CHECK("attention_tiles");
+    if (plan.parts > 1) {
+        constexpr int PER = 256 / (HD / 4);
+        hipLaunchKernelGGL((attention_merge_kernel<T, HD>), dim3((unsigned)(((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER)), dim3(256), 0, st, p);
+        VF_LAUNCH_CHECK("attention_merge");
+    }
     return VF_OK;
 }
 
@@ -84,27 +400,39 @@ extern "C" {
 
 size_t vf_attention_packed_workspace(const vf_packed_args *args) {
     if (check("vf_attention_packed_workspace", args) != VF_OK) return (size_t)-1;
-    return 0;
+    return make_plan(*args).bytes;
 }
 
 int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const void *kv_layer_dev, const int32_t *block_table_dev,
                         const int32_t *row_off_dev, const int32_t *kv_len_dev, void *out_dev, void *workspace_dev, size_t workspace_bytes,
                         void *stream) {
     if (int rc = check("vf_attention_packed", args)) return rc;
-    PackedAttn p = {*args, q_dev, kv_layer_dev, block_table_dev, row_off_dev, kv_len_dev, out_dev};
+    PackedAttn p = {};
+    p.a = *args;
     if (p.a.total_rows == 0) return VF_OK;
     if (!q_dev || !kv_layer_dev || !block_table_dev || !row_off_dev || !kv_len_dev || !out_dev)
         return vf_fail(VF_ERR_ARG, "vf_attention_packed: NULL argument");
-    if (((uintptr_t)q_dev | (uintptr_t)kv_layer_dev | (uintptr_t)out_dev) & 15)
+    if (((uintptr_t)q_dev | (uintptr_t)kv_layer_dev | (uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15)
         return vf_fail(VF_ERR_UNSUPPORTED, "vf_attention_packed: addresses are multiples of 16 bytes");
-    if (p.a.scale == 0.f) p.a.scale = 1.0f / sqrtf((float)p.a.head_dim);
-    hipStream_t st = (hipStream_t)stream;
-    const dim3 grid(p.a.total_rows, p.a.n_q_heads);
-    const auto kernel = p.a.dtype == VF_BF16 ? (p.a.head_dim == 128 ? attention_plain_kernel<bf16_t, 128> : attention_plain_kernel<bf16_t, 64>)
-                                             : (p.a.head_dim == 128 ? attention_plain_kernel<float, 128> : attention_plain_kernel<float, 64>);
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, st, p);
-    VF_LAUNCH_CHECK("attention_packed");
-    return VF_OK;
+    const Plan plan = make_plan(p.a);
+    if (plan.bytes && !workspace_dev) return vf_fail(VF_ERR_ARG, "vf_attention_packed: needs a workspace of %zu bytes", plan.bytes);
+    if (plan.bytes > workspace_bytes) return vf_fail(VF_ERR_CAP, "vf_attention_packed: workspace of %zu bytes, needs %zu", workspace_bytes, plan.bytes);
+    p.q = q_dev;
+    p.kv = kv_layer_dev;
+    p.table = block_table_dev;
+    p.row_off = row_off_dev;
+    p.kv_len = kv_len_dev;
+    p.out = out_dev;
+    p.group = p.a.n_q_heads / p.a.n_kv_heads;
+    p.tiles = plan.tiles;
+    p.parts = plan.parts;
+    p.part_pages = plan.part_pages;
+    p.scale_log2e = (p.a.scale == 0.f ? 1.0f / sqrtf((float)p.a.head_dim) : p.a.scale) * 1.4426950408889634f;
+    p.records = (float *)workspace_dev;
+    p.used = (int32_t *)((char *)workspace_dev + plan.bytes - (size_t)p.a.total_rows * sizeof(int32_t));
+    const auto go = p.a.dtype == VF_BF16 ? (p.a.head_dim == 128 ? launch<bf16_t, 128> : launch<bf16_t, 64>)
+                                         : (p.a.head_dim == 128 ? launch<float, 128> : launch<float, 64>);
+    return go(p, plan, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -206,6 +206,8 @@ template <typename T> __device__ inline T from_f32(float v);
 template <> __device__ inline float from_f32<float>(float v) { return v; }
 template <> __device__ inline bf16_t from_f32<bf16_t>(float v) { return (bf16_t)v; }  // round-to-nearest-even
 
+template <typename T> struct alignas(16) Eight { T v[8]; };   // eight elements, moved as one or two 16-byte pieces
+
 // Kernels that keep MFMA accumulators live across a loop ask for at least two wavefronts per SIMD:
 // within that register budget (256 per lane) the compiler places accumulators in ordinary vector
 // registers and updates them in place; with the whole file at its disposal it moves them to and

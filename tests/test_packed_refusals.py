@@ -84,7 +84,7 @@ def _attn(**kw):
     (dict(n_q_heads=512), vf.VF_ERR_ARG), (dict(head_dim=80), vf.VF_ERR_UNSUPPORTED), (dict(n_seqs=0), vf.VF_ERR_ARG),
     (dict(n_seqs=vf.VF_PACKED_MAX_SEQS + 1), vf.VF_ERR_ARG), (dict(total_rows=-1), vf.VF_ERR_ARG), (dict(max_rows=-1), vf.VF_ERR_ARG),
     (dict(max_keys=-1), vf.VF_ERR_ARG), (dict(pool_pages=0), vf.VF_ERR_ARG), (dict(max_pages=0), vf.VF_ERR_ARG),
-    (dict(table_stride=1), vf.VF_ERR_ARG), (dict(scale=float("nan")), vf.VF_ERR_ARG), (dict(q_stride=255), vf.VF_ERR_ARG),
+    (dict(table_stride=1), vf.VF_ERR_ARG), (dict(scale=float("nan")), vf.VF_ERR_ARG), (dict(scale=-1.0), vf.VF_ERR_ARG), (dict(q_stride=255), vf.VF_ERR_ARG),
     (dict(out_stride=260), vf.VF_ERR_UNSUPPORTED)])
 def test_attention(kw, code):
     a = _attn(**kw)
@@ -99,3 +99,11 @@ def test_attention_null_alignment_and_empty():
     assert L.vf_attention_packed(C.byref(a), C.c_void_p(4100), *[P] * 6, 1 << 30, None) == vf.VF_ERR_UNSUPPORTED
     assert L.vf_attention_packed(None, *[P] * 7, 0, None) == vf.VF_ERR_ARG
     assert L.vf_attention_packed(C.byref(_attn(total_rows=0)), *[None] * 7, 0, None) == vf.VF_OK
+
+def test_workspace_too_small_is_refused():
+    # one token over a long context: its keys are split and meet in the workspace
+    a = _attn(n_seqs=1, total_rows=1, max_rows=1, max_keys=100_000, pool_pages=2000, max_pages=2000, table_stride=2000)
+    need = L.vf_attention_packed_workspace(C.byref(a))
+    assert 0 < need < 1 << 30
+    assert L.vf_attention_packed(C.byref(a), *[P] * 7, need - 1, None) == vf.VF_ERR_CAP
+    assert L.vf_attention_packed(C.byref(a), *[P] * 6, None, need, None) == vf.VF_ERR_ARG

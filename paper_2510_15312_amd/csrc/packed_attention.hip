@@ -109,7 +109,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     const int row = t.row0 + item / group, head = kvh * group + item % group;
     const int last_key = min(first_pos + item / group, cap - 1);
     const int tile_last = min(first_pos + min(n_items - 1, t.item0 + BM - 1) / group, cap - 1);
-    const int wave_last = wave0 < n_items ? min(first_pos + min(n_items - 1, wave0 + 31) / group, cap - 1) : -1;
+    const bool has_items = wave0 < n_items;   // a wavefront without items still brings its share of the pages
+    const int wave_last = has_items ? min(first_pos + min(n_items - 1, wave0 + 31) / group, cap - 1) : -1;
     const int wave_first = min(first_pos + min(n_items - 1, wave0) / group, cap - 1);
     const int pages = tile_last < 0 ? 0 : tile_last / VF_TILE + 1;
     const int p_begin = part * p.part_pages, p_end = part == p.parts - 1 ? pages : min(pages, p_begin + p.part_pages);
@@ -142,17 +143,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
         const int id = __builtin_amdgcn_readlane(ids, pg - ids_at);
         return (unsigned)id < (unsigned)a.pool_pages ? id : -1;
     };
-    unsigned long long there = 0;   // bit i: page i (mod 64) of the ring is in the pool
+    // K of page i + 1 and V of page i travel together, one step ahead of their use: a wavefront brings K or V
     auto issue = [&](int i) {
-        const int pg = p_begin + i;
-        if (pg >= p_end) {   // nothing to load; the count of loads in flight stays what the waits assume
-            static_for<0, LPW>([&](auto f) { fragment_to_lds<(int)f * 1024>(src, lane * 16, lds0 + (unsigned)i % S * (UNITS * 1024)); });
-            return;
-        }
-        const int id = page_id(pg);
-        there = (there & ~(1ull << (i & 63))) | (unsigned long long)(id >= 0) << (i & 63);
+        const int pg = p_begin + i + (wave < WAVES / 2 ? 1 : 0);
+        const int id = page_id(max(p_begin, min(pg, p_end - 1)));   // a page that is not needed: some page, not used
         const char *from = src + (size_t)max(id, 0) * page_bytes;
-        const unsigned dst = lds0 + (unsigned)i % S * (UNITS * 1024);
+        const unsigned dst = lds0 + (unsigned)(pg & 1) * (UNITS * 1024);
         static_for<0, LPW>([&](auto f) {
             constexpr int F = f;
             if constexpr (HALVES == 1) fragment_to_lds<F * 1024>(from + F * 1024, lane * 16, dst);
@@ -184,27 +180,24 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
     float m_run = -1e30f, l_run = 0.f;   // l_run: this lane's keys
-    auto update = [&](const unsigned char *st, int t0, auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        floatx16 sc[2];
+    struct Scores { floatx16 t[2]; };   // 32 keys each: register i of t[kt] is key 32 kt + 16 (i >> 3) + 8 half + (i & 7) of the page
+    auto scores = [&](const unsigned char *st) {
+        Scores sc;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[kt][i] = 0.f;
+            for (int i = 0; i < 16; ++i) sc.t[kt][i] = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) sc[kt] = mma(k_piece(st, kt, s), qf[s], sc[kt]);
-        const int own = t0 + half * 8;   // key of register i of tile kt: own + 32 kt + 16 (i >> 3) + (i & 7)
-        if constexpr (MASKED)
+            for (int kt = 0; kt < 2; ++kt) sc.t[kt] = mma(k_piece(st, kt, s), qf[s], sc.t[kt]);
+        return sc;
+    };
+    Frag<T> w[4];
+    auto weights = [&](const Scores &sc) {
+        float mx = sc.t[0][0];
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (own + kt * 32 + (i >> 3) * 16 + (i & 7) > last_key) sc[kt][i] = -INFINITY;
-        float mx = sc[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
+        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc.t[i >> 4][i & 15]);
         mx = halves_max(mx) * p.scale_log2e;
         // The weights' common factor follows the maximum with slack: they stay below 2^8, and the sums are rescaled in few pages.
         if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
@@ -214,68 +207,126 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             for (int db = 0; db < DB; ++db) acc[db] *= keep;
             m_run = m_new;
         }
-        Frag<T> w[4];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(sc[i >> 4][i & 15], p.scale_log2e, -m_run));
-            l_run += x;
+            const float x = __builtin_amdgcn_exp2f(fmaf(sc.t[i >> 4][i & 15], p.scale_log2e, -m_run));
+            if constexpr (HALVES == 2) l_run += x;
             w[i >> 3].v[i & 7] = from_f32<T>(x);
         }
-        // O^T += V^T W^T of 32 output dimensions; MASKED: keys beyond `seen` are taken as zeros
-        auto product = [&](auto db, int seen, floatx16 c) {
+        // the sum is that of the rounded weights, which the products take
+        if constexpr (HALVES == 1)
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int i = 0; i < 32; i += 2) {
+                typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[i >> 3].v[i & 7], w[i >> 3].v[(i & 7) + 1]}, bf16x2{(bf16_t)1.f, (bf16_t)1.f}, l_run, false);
+            }
+    };
+    auto products = [&](const unsigned char *st) {   // O^T += V^T W^T
 #pragma unroll
-                for (int tt = 0; tt < 2; ++tt) {
-                    Frag<T> v = v_piece(st, kt, tt, db);
-                    if constexpr (MASKED)
+        for (int g = 0; g < 4; ++g)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (own + kt * 32 + tt * 16 + j > seen) v.v[j] = from_f32<T>(0.f);
-                    c = mma(v, w[kt * 2 + tt], c);
-                }
+            for (int db = 0; db < DB; ++db) acc[db] = mma(v_piece(st, g / 2, g % 2, db), w[g], acc[db]);
+    };
+    // the same where some keys are not seen by all items
+    auto products_masked = [&](const unsigned char *st, int t0) {
+        const int own = t0 + half * 8, page_last = min(wave_last, t0 + VF_TILE - 1);
+        auto product = [&](auto db, int seen, floatx16 c) {   // keys beyond `seen` are taken as zeros
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                Frag<T> v = v_piece(st, g / 2, g % 2, db);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (own + g * 16 + j > seen) v.v[j] = from_f32<T>(0.f);
+                c = mma(v, w[g], c);
+            }
             return c;
         };
         static_for<0, DB>([&](auto db) {
             constexpr int D = db;
-            if constexpr (MASKED) {
-                // 0 times a value that is not finite is not 0: keys beyond all items count as zeros, and if a key that only some
-                // items see holds such a value, every row takes the product with its own keys
-                bool bad = false;
+            // 0 times a value that is not finite is not 0: keys beyond all items count as zeros, and if a key that only some
+            // items see holds such a value, every row takes the product with its own keys
+            bool bad = false;
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+            for (int g = 0; g < 4; ++g) {
+                const Frag<T> v = v_piece(st, g / 2, g % 2, D);
 #pragma unroll
-                    for (int tt = 0; tt < 2; ++tt) {
-                        const Frag<T> v = v_piece(st, kt, tt, D);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) bad |= own + kt * 32 + tt * 16 + j <= wave_last && not_finite(to_f32(v.v[j]));
-                    }
-                if (__builtin_amdgcn_ballot_w64(bad)) {
-                    floatx16 sum = acc[D];   // of rows that see nothing here
-                    for (int seen = max(wave_first, t0); seen <= min(wave_last, t0 + VF_TILE - 1); ++seen) {
-                        const floatx16 c = product(db, seen, acc[D]);
-                        if (min(last_key, t0 + VF_TILE - 1) == seen) sum = c;
-                    }
-                    acc[D] = sum;
-                    return;
-                }
+                for (int j = 0; j < 8; ++j) bad |= own + g * 16 + j <= page_last && not_finite(to_f32(v.v[j]));
             }
-            acc[D] = product(db, wave_last, acc[D]);
+            if (!__builtin_amdgcn_ballot_w64(bad)) {
+                acc[D] = product(db, page_last, acc[D]);
+            } else {
+                floatx16 sum = acc[D];   // of rows that see nothing here
+                for (int seen = max(wave_first, t0); seen <= page_last; ++seen) {
+                    const floatx16 c = product(db, seen, acc[D]);
+                    if (min(last_key, t0 + VF_TILE - 1) == seen) sum = c;
+                }
+                acc[D] = sum;
+            }
+            __builtin_amdgcn_sched_barrier(0);   // one block's values in registers at a time
         });
     };
+    // Steps: page i's weights and products, and the scores of page i + 1, which do not wait for them.
     const int n = p_end - p_begin;
     if (n > 0) {
+        // pages that all items see whole, up to the first that is not in the pool
+        int n_full = max(0, min(n, (min(first_pos + t.item0 / group, cap - 1) + 1) / VF_TILE - p_begin));
+        for (int i0 = 0; i0 < n_full; i0 += 64) {
+            const unsigned long long missing = __builtin_amdgcn_ballot_w64((unsigned)table[p_begin + min(i0 + lane, n_full - 1)] >= (unsigned)a.pool_pages);
+            if (missing) n_full = min(n_full, i0 + __builtin_ctzll(missing));
+        }
+        auto k_page = [&](int i) { return smem + ((p_begin + i) & 1) * (UNITS * 1024); };
+        auto step = [&](int i) {   // behind it K of page i + 1 and V of page i have landed, and their slots' neighbours are free
+            vm_wait<0>();
+            lds_sync();
+            issue(i + 1);
+        };
+        issue(-1);
+        vm_wait<0>();
+        lds_sync();
+        issue(0);
+        if (!has_items) {
+            for (int i = 0; i < n; ++i) step(i);
+        } else {
+            int i = 0;
+            if (n_full > 0) {
+                Scores even = scores(k_page(0)), odd;
+                auto last = [&](const Scores &sc) {
+                    step(i);
+                    weights(sc);
+                    products(k_page(i));
+                    ++i;
+                };
+                auto next = [&](const Scores &sc, Scores &ahead) {
+                    step(i);
+                    ahead = scores(k_page(i + 1));
+                    weights(sc);
+                    products(k_page(i));
+                    ++i;
+                };
+                while (i + 2 < n_full) {
+                    next(even, odd);
+                    next(odd, even);
+                }
+                if (i + 1 < n_full) {
+                    next(even, odd);
+                    last(odd);
+                } else {
+                    last(even);
+                }
+            }
+            for (; i < n; ++i) {
+                const int t0 = (p_begin + i) * VF_TILE;
+                const bool mine = t0 <= wave_last && page_id(p_begin + i) >= 0;
+                Scores sc;
+                if (mine) sc = scores(k_page(i));
+                step(i);
+                if (!mine) continue;
 #pragma unroll
-        for (int i = 0; i < S - 1; ++i) issue(i);
-        for (int i = 0; i < n; ++i) {
-            vm_wait<(S - 2) * LPW>();   // page i has landed; behind the barrier everyone's share of it has,
-            lds_sync();                 // and page i - 1 has been read, so its slot takes page i + S - 1
-            issue(i + S - 1);
-            const int t0 = (p_begin + i) * VF_TILE;
-            const unsigned char *st = smem + (unsigned)i % S * (UNITS * 1024);
-            if (t0 > wave_last || !(there >> (i & 63) & 1)) continue;
-            if (t0 + VF_TILE - 1 <= wave_first) update(st, t0, std::false_type{});
-            else update(st, t0, std::true_type{});
+                for (int j = 0; j < 32; ++j)
+                    if (t0 + half * 8 + (j >> 3) * 16 + (j & 7) > last_key) sc.t[j >> 4][j & 15] = -INFINITY;
+                weights(sc);
+                products_masked(k_page(i), t0);
+            }
         }
         vm_wait<0>();   // nothing is on its way to LDS when the workgroup ends
     }

@@ -87,11 +87,11 @@ template <typename T> __device__ __forceinline__ bool any_not_finite(const Frag<
 
 // Tiles of 32 items a wavefront, pages of 64 keys through LDS.
 //
-// A page comes as direct loads of 1 KB units, S - 1 pages ahead.  Units hold 16 bytes a lane: a K or V piece of eight elements
+// A page comes as direct loads of 1 KB units.  Units hold 16 bytes a lane: a K or V piece of eight elements
 // in bfloat16, half of one in float32 (the halves of a fragment's pieces in two units, so that a read of 16 bytes a lane
 // touches every bank once).  K rows are taken in the order that leaves a lane with eight consecutive keys per operand of
 // the second product: row m of a 32-key tile is key 16 (m >> 4) + 8 (m >> 2 & 1) + 4 (m >> 3 & 1) + (m & 3).
-template <typename T, int HD, int WAVES, int S>
+template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAttn p) {
     constexpr int BM = WAVES * 32, HALVES = sizeof(T) / 2, UNITS = HD / 4 * HALVES, LPW = UNITS / WAVES;   // units of a page
     constexpr int KD = HD / 32, KS = HD / 16, DB = HD / 32;
@@ -358,6 +358,228 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
         }
 }
 
+// Few items of a sequence (single tokens, short drafts): a workgroup takes 16 NB items at a time of one sequence and key head over
+// one part of the keys, its wavefronts the part's tiles of 32 keys in turn, straight from memory into registers: every K and V
+// fragment of the pool is one contiguous kilobyte.  The wavefronts' sums meet in LDS.
+// Operands of a 16x16 product over 32 values of k: 16 lanes each take 8.
+__device__ __forceinline__ floatx4 mma16(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 mma16(const Frag<float> &a, const Frag<float> &b, floatx4 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
+template <typename T> __device__ __forceinline__ Frag<T> load_frag(const char *at) {
+    Frag<T> f;
+    const Eight<T> x = *reinterpret_cast<const Eight<T> *>(at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j] = x.v[j];
+    return f;
+}
+
+template <typename T, int HD, int WAVES, int NB>
+__global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kernel(PackedAttn p) {
+    constexpr int KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = 16 * NB, OUT = HD + 1;   // FRAG: bytes; OUT: stride of a sum in LDS
+    extern __shared__ __align__(16) float sums[];   // [WAVES][BM][OUT], then maxima and sums of weights
+    float *maxima = sums + WAVES * BM * OUT, *totals = maxima + WAVES * BM;
+    const vf_packed_args &a = p.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4, l15 = lane & 15;
+    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % p.parts, seq = rest / p.parts;
+    const int p_first = part * p.part_pages;
+    const int32_t *table = p.table + (size_t)seq * a.table_stride;
+    int ids = table[min(p_first + lane, a.max_pages - 1)];   // asked for with the lengths
+    const int2 r = seq_rows(p, seq);
+    const int row0 = __builtin_amdgcn_readfirstlane(r.x), rows = __builtin_amdgcn_readfirstlane(r.y), kv_len = __builtin_amdgcn_readfirstlane(p.kv_len[seq]);
+    const int group = p.group, n_items = rows * group, cap = min(kv_len, a.max_pages * VF_TILE), first_pos = kv_len - rows;
+    const size_t page_bytes = (size_t)2 * a.n_kv_heads * VF_TILE * HD * sizeof(T), head_bytes = (size_t)VF_TILE * HD * sizeof(T);
+    for (int item0 = 0; item0 < n_items; item0 += BM) {
+        const int last = min(first_pos + min(n_items - 1, item0 + BM - 1) / group, cap - 1);   // last key that an item sees
+        const int pages = last < 0 ? 0 : last / VF_TILE + 1, parts = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
+        const int p_end = part == p.parts - 1 ? pages : min(pages, p_first + p.part_pages);
+        if (p.parts > 1 && part == 0 && kvh == 0 && threadIdx.x < BM && item0 + (int)threadIdx.x < n_items)
+            p.used[row0 + (item0 + threadIdx.x) / group] = parts;
+        if (p_first >= p_end && part > 0) continue;
+        int last_key[NB];
+        Frag<T> qf[NB][KD];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int item = min(n_items - 1, item0 + nb * 16 + l15);
+            last_key[nb] = min(first_pos + item / group, cap - 1);
+            const T *q = (const T *)p.q + (row0 + item / group) * a.q_stride + (kvh * group + item % group) * HD + g4 * 8;
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd) qf[nb][kd] = load_frag<T>((const char *)(q + kd * 32));
+        }
+        floatx4 acc[NB][DB];
+        float m_run[NB], l_run[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            m_run[nb] = -1e30f;
+            l_run[nb] = 0.f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[nb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        // keys 32 i .. + 31, i = 2 p_first + wave, + WAVES ..
+        const int first_all = min(first_pos + item0 / group, cap - 1);   // last key that all items see
+        const int i_end = min(2 * p_end, last / 32 + 1);
+        int ids_at = p_first;
+        Frag<T> k[2 * KD], v[DB];   // a tile's keys are asked for when those before have been multiplied, its values likewise
+        auto page = [&](int i) {    // page id of tile i, -1: not in the pool
+            const int pg = i / 2;
+            if (pg - ids_at >= 64) {
+                ids_at = pg;
+                ids = table[min(pg + lane, a.max_pages - 1)];
+            }
+            const int id = __builtin_amdgcn_readlane(ids, pg - ids_at);
+            return (unsigned)id < (unsigned)a.pool_pages ? id : -1;
+        };
+        const char *kv = (const char *)p.kv + kvh * head_bytes + lane * 8 * sizeof(T);
+        auto load_k = [&](int i, int id) {
+            const char *at = kv + (size_t)max(id, 0) * page_bytes + (i & 1) * (KD * 2 * FRAG);
+#pragma unroll
+            for (int f = 0; f < 2 * KD; ++f) k[f] = load_frag<T>(at + f * FRAG);
+        };
+        auto load_v = [&](int i, int id) {
+            const char *at = kv + (size_t)max(id, 0) * page_bytes + a.n_kv_heads * head_bytes + (i & 1) * (DB * FRAG);
+#pragma unroll
+            for (int f = 0; f < DB; ++f) v[f] = load_frag<T>(at + f * FRAG);
+        };
+        int id = -1;
+        if (2 * p_first + wave < i_end) {
+            id = page(2 * p_first + wave);
+            load_k(2 * p_first + wave, id);
+            load_v(2 * p_first + wave, id);
+        }
+        for (int i = 2 * p_first + wave, id_next; i < i_end; i += WAVES, id = id_next) {
+            const int i_next = min(i + WAVES, i_end - 1);   // past the end: the last tile again, not used
+            id_next = page(i_next);
+            const int own = i * 32 + g4 * 8;                // key of score j: own + j
+            const bool masked = i * 32 + 31 > first_all;
+            float s[NB][8];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                floatx4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) c[h] = mma16(k[h * KD + kd], qf[nb][kd], c[h]);
+                float mx = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    s[nb][j] = id < 0 || (masked && own + j > last_key[nb]) ? -INFINITY : c[j >> 2][j & 3];
+                    mx = fmaxf(mx, s[nb][j]);
+                }
+                mx *= p.scale_log2e;
+                if (__builtin_amdgcn_ballot_w64(mx > m_run[nb] + 8.f)) {   // with slack: see attention_tiles_kernel
+                    mx = over_item(mx, [](float u, float v) { return fmaxf(u, v); });
+                    const float m_new = fmaxf(m_run[nb], mx), keep = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
+                    l_run[nb] *= keep;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) acc[nb][db] *= keep;
+                    m_run[nb] = m_new;
+                }
+            }
+            load_k(i_next, id_next);
+            // values of keys that nobody sees count as zeros; one that only some items see and that is not finite would reach
+            // the others as 0 times it: then each row takes the product with its own keys
+            bool bad = false;
+            if (masked || id < 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        if (id < 0 || own + j > last) v[db].v[j] = from_f32<T>(0.f);
+                        bad |= own + j > first_all && not_finite(to_f32(v[db].v[j]));
+                    }
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                // bfloat16 weights as a sum of two (16 significant bits): the loads, not the products, are what this kernel waits for.
+                // The first is rounded towards zero and the second never zero beside it, so that an infinite value stays one.
+                Frag<T> hi, lo;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float w = __builtin_amdgcn_exp2f(fmaf(s[nb][j], p.scale_log2e, -m_run[nb]));
+                    l_run[nb] += w;
+                    if constexpr (sizeof(T) == 2) {
+                        const float top = __uint_as_float(__float_as_uint(w) & 0xffff0000u);
+                        hi.v[j] = from_f32<T>(top);
+                        lo.v[j] = from_f32<T>(fmaxf(w - top, w * 0x1p-24f));
+                    } else {
+                        hi.v[j] = w;
+                    }
+                }
+                auto product = [&](const Frag<T> &x, floatx4 c) {
+                    c = mma16(x, hi, c);
+                    if constexpr (sizeof(T) == 2) c = mma16(x, lo, c);
+                    return c;
+                };
+                if (!__builtin_amdgcn_ballot_w64(bad)) {
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) acc[nb][db] = product(v[db], acc[nb][db]);
+                } else {
+                    static_for<0, DB>([&](auto db) {
+                        floatx4 sum = acc[nb][(int)db];
+                        for (int seen = max(first_all, i * 32); seen <= min(last, i * 32 + 31); ++seen) {
+                            Frag<T> x = v[(int)db];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (own + j > seen) x.v[j] = from_f32<T>(0.f);
+                            const floatx4 c = product(x, acc[nb][(int)db]);
+                            if (min(last_key[nb], i * 32 + 31) == seen) sum = c;
+                        }
+                        acc[nb][(int)db] = sum;
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                }
+            }
+            load_v(i_next, id_next);
+        }
+        // sums of the wavefronts; a lane's values: item l15, d = 16 db + 4 g4 + r
+        if (item0) __syncthreads();
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float l = l_run[nb];
+            l = over_item(l, [](float u, float v) { return u + v; });
+            const int at = wave * BM + nb * 16 + l15;
+            if (g4 == 0) { maxima[at] = m_run[nb]; totals[at] = l; }
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums[at * OUT + db * 16 + g4 * 4 + e] = acc[nb][db][e];
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j < BM * (HD / 4); j += WAVES * 64) {
+            const int it = j / (HD / 4), d0 = j % (HD / 4) * 4, item = item0 + it;
+            if (item >= n_items) break;
+            float M = -1e30f, L = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) M = fmaxf(M, maxima[w * BM + it]);
+            floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float f = __builtin_amdgcn_exp2f(maxima[w * BM + it] - M);
+                L += totals[w * BM + it] * f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += sums[(w * BM + it) * OUT + d0 + e] * f;
+            }
+            const int row = row0 + item / group, head = kvh * group + item % group;
+            if (p.parts > 1) {
+                float *rec = p.records + (((size_t)row * a.n_q_heads + head) * p.parts + part) * (REC_HEAD + HD);
+                if (d0 == 0) *reinterpret_cast<float2 *>(rec) = float2{M, L};
+                *reinterpret_cast<floatx4 *>(rec + REC_HEAD + d0) = o;
+            } else {
+                const float inv = L == 0.f ? 0.f : 1.0f / L;
+                typedef T four __attribute__((ext_vector_type(4)));
+                four x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = from_f32<T>(o[e] * inv);
+                *reinterpret_cast<four *>((T *)p.out + row * a.out_stride + head * HD + d0) = x;
+            }
+        }
+    }
+}
+
 // Merge of the parts: HD / 4 threads per row and head.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
@@ -409,18 +631,27 @@ int check(const char *name, const vf_packed_args *args) {
 }
 
 // Kernel, tiles and parts of a call, from what the host knows.
-struct Plan { int waves, tiles, parts, part_pages; size_t bytes; };
+struct Plan { int few, tiles, parts, part_pages; size_t bytes; };   // few: blocks of 16 items of attention_few_kernel, 0: attention_tiles_kernel
+
+constexpr int TILE_WAVES = 4, FEW_WAVES = 8;
 
 Plan make_plan(const vf_packed_args &a) {
     Plan r{};
     const int group = a.n_q_heads / a.n_kv_heads;
-    r.waves = 4;
-    const int bm = r.waves * 32;
-    const long long items = (long long)a.total_rows * group;
-    r.tiles = (int)(items / bm + std::min(a.n_seqs, a.total_rows));   // a sequence ends in one tile that is not full
-    const int pages = std::max(1, std::min(a.max_pages, (a.max_keys + VF_TILE - 1) / VF_TILE));
-    const long long groups = (long long)std::max<long long>(1, std::min<long long>(r.tiles, (items + bm - 1) / bm)) * a.n_kv_heads;
-    r.parts = (int)std::max(1ll, std::min<long long>((512 + groups - 1) / groups, pages / 4));
+    const int pages = std::max(1, std::min(a.max_pages, (int)(((long long)a.max_keys + VF_TILE - 1) / VF_TILE)));
+    const long long most_items = (long long)std::min(a.max_rows, a.total_rows) * group, items = (long long)a.total_rows * group;
+    long long groups;
+    if (most_items <= (a.head_dim == 64 ? 32 : 16)) {
+        r.few = most_items <= 16 ? 1 : 2;
+        r.tiles = a.n_seqs;
+        groups = (long long)std::min(a.n_seqs, a.total_rows) * a.n_kv_heads;
+        r.parts = (int)std::max(1ll, std::min<long long>((512 + groups - 1) / groups, pages / 8));
+    } else {
+        const int bm = TILE_WAVES * 32;
+        r.tiles = (int)(items / bm + std::min(a.n_seqs, a.total_rows));   // a sequence ends in one tile that is not full
+        groups = std::max<long long>(1, std::min<long long>(r.tiles, (items + bm - 1) / bm)) * a.n_kv_heads;
+        r.parts = (int)std::max(1ll, std::min<long long>((512 + groups - 1) / groups, pages / 4));
+    }
     r.part_pages = (pages + r.parts - 1) / r.parts;
     r.parts = (pages + r.part_pages - 1) / r.part_pages;
     if (r.parts > 1)
@@ -428,21 +659,29 @@ Plan make_plan(const vf_packed_args &a) {
     return r;
 }
 
-template <typename T, int HD>
-int launch(PackedAttn &p, const Plan &plan, hipStream_t st) {
-    constexpr int WAVES = 4, S = 2, LDS = S * HD / 4 * 1024 * (int)sizeof(T) / 2;
-    static const hipError_t set = hipFuncSetAttribute((const void *)attention_tiles_kernel<T, HD, WAVES, S>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    VF_HIP(set);
-    const long long blocks = (long long)plan.tiles * plan.parts * p.a.n_kv_heads;
+template <typename F> int start(F kernel, long long blocks, int threads, int lds, const PackedAttn &p, hipStream_t st) {
     if (blocks > 0x7fffff) return vf_fail(VF_ERR_UNSUPPORTED, "vf_attention_packed: %lld workgroups", blocks);
-    hipLaunchKernelGGL((attention_tiles_kernel<T, HD, WAVES, S>), dim3((unsigned)blocks), dim3(WAVES * 64), LDS, st, p);
-    VF_LAUNCH_CHECK("attention_tiles");
-    if (plan.parts > 1) {
-        constexpr int PER = 256 / (HD / 4);
-        hipLaunchKernelGGL((attention_merge_kernel<T, HD>), dim3((unsigned)(((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER)), dim3(256), 0, st, p);
-        VF_LAUNCH_CHECK("attention_merge");
-    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, st, p);
+    VF_LAUNCH_CHECK("attention_packed");
     return VF_OK;
+}
+template <typename T, int HD, int NB> int launch_few(const PackedAttn &p, hipStream_t st) {
+    constexpr int LDS = FEW_WAVES * 16 * NB * (HD + 3) * 4;
+    static const hipError_t set = hipFuncSetAttribute((const void *)attention_few_kernel<T, HD, FEW_WAVES, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    VF_HIP(set);
+    return start(attention_few_kernel<T, HD, FEW_WAVES, NB>, (long long)p.a.n_seqs * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
+}
+template <typename T, int HD> int launch_tiles(const PackedAttn &p, hipStream_t st) {
+    constexpr int LDS = 2 * HD / 4 * 1024 * (int)sizeof(T) / 2;
+    static const hipError_t set = hipFuncSetAttribute((const void *)attention_tiles_kernel<T, HD, TILE_WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    VF_HIP(set);
+    return start(attention_tiles_kernel<T, HD, TILE_WAVES>, (long long)p.tiles * p.parts * p.a.n_kv_heads, TILE_WAVES * 64, LDS, p, st);
+}
+template <typename T, int HD> int launch(const PackedAttn &p, const Plan &plan, hipStream_t st) {
+    const int rc = plan.few == 1 ? launch_few<T, HD, 1>(p, st) : plan.few == 2 ? launch_few<T, HD, HD == 64 ? 2 : 1>(p, st) : launch_tiles<T, HD>(p, st);
+    if (rc != VF_OK || p.parts == 1) return rc;
+    constexpr int PER = 256 / (HD / 4);
+    return start(attention_merge_kernel<T, HD>, ((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER, 256, 0, p, st);
 }
 
 }  // namespace

@@ -151,6 +151,12 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _stream_of(t):
+    """The current stream of the tensor's device as an address.  A step's packed calls take a few microseconds each: through
+    the stream object this alone is 2.8 of them, like this 0.1."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
 def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
@@ -406,40 +412,50 @@ def _refuse(what):
     raise VfError(VF_ERR_ARG, what)
 
 
+_I32 = torch.int32
+
+
 def _ints(name, t, n):
     """The address of an int32 device tensor of at least n entries one behind the other."""
-    if t.dtype != torch.int32 or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not _I32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
         _refuse(f"{name}: contiguous int32 device tensor of {n} entries")
     return t.data_ptr()
 
 
 def _rows(name, t, dtype, rows, heads, hd):
     """The row stride of a device tensor [rows, heads, hd] whose rows are contiguous."""
-    if t.dtype != dtype or t.shape != (rows, heads, hd) or not t.is_cuda or t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd):
-        _refuse(f"{name}: device tensor [{rows}, {heads}, {hd}] of {dtype} with contiguous rows")
-    return t.stride(0) if rows > 1 else max(t.stride(0), heads * hd)
+    if t.dtype is not dtype or t.shape != (rows, heads, hd) or not t.is_cuda:
+        _refuse(f"{name}: device tensor [{rows}, {heads}, {hd}] of {dtype}")
+    row, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != hd):
+        _refuse(f"{name}: rows that are contiguous")
+    return row if rows > 1 else max(row, heads * hd)
 
 
 def _pool(t, hd, dtype):
     """(pages, kv heads) of one layer's pages, [pages, 2, kv heads, 64 * hd]."""
-    if t.dim() != 4 or t.shape[1] != 2 or t.shape[3] != 64 * hd or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+    s = t.shape
+    if len(s) != 4 or s[1] != 2 or s[3] != 64 * hd or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda:
         _refuse(f"pool: contiguous device tensor [pages, 2, kv heads, {64 * hd}] of {dtype}")
-    return t.shape[0], t.shape[2]
+    return s[0], s[2]
 
 
 def _table(t):
     """(sequences, entries a sequence, stride) of a block table."""
-    if t.dim() != 2 or t.dtype != torch.int32 or t.stride(1) != 1 or not t.is_cuda:
+    if t.dim() != 2 or t.dtype is not _I32 or not t.is_cuda:
         _refuse("block table: int32 device tensor [sequences, pages]")
-    n, m = t.shape
-    return n, m, t.stride(0) if n > 1 else max(t.stride(0), m)
+    (n, m), (row, one) = t.shape, t.stride()
+    if one != 1 and m > 1:
+        _refuse("block table: rows that are contiguous")
+    return n, m, row if n > 1 else max(row, m)
 
 
 _DTYPES = {torch.bfloat16: VF_BF16, torch.float32: VF_F32}
 
 
 def _dtype(t):
-    return _DTYPES[t.dtype] if t.dtype in _DTYPES else _refuse(f"dtype {t.dtype}")
+    code = _DTYPES.get(t.dtype)
+    return _refuse(f"dtype {t.dtype}") if code is None else code
 
 
 def kv_layer(model, pool, layer):
@@ -458,7 +474,7 @@ def vf_pages_assign(lens, new, free_pages, n_free, block_table, row_off, pos, sl
     _check(lib.vf_pages_assign(n, m, stride, rows, free_pages.numel(), _ints("lens", lens, n), _ints("new", new, n),
                                _ints("free_pages", free_pages, 0), _ints("n_free", n_free, 1), block_table.data_ptr(),
                                _ints("row_off", row_off, n + 1), _ints("pos", pos, rows), _ints("slot", slot, rows),
-                               _ints("kv_len", kv_len, n), _ints("n_free_out", n_free_out, 1), _stream()))
+                               _ints("kv_len", kv_len, n), _ints("n_free_out", n_free_out, 1), _stream_of(lens)))
 
 
 def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED, factor=1.0, low=0.0, high=0.0, trained=0.0,
@@ -466,7 +482,7 @@ def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED
     """float32 [max_positions, rotary_dim / 2, 2]: cos and sin of every position's angles."""
     plan = vf_rotary_plan(int(rotary_dim), int(max_positions), int(scaling), 0, theta, factor, low, high, trained, magnitude)
     table = torch.empty((max(int(max_positions), 0), max(int(rotary_dim), 0) // 2, 2), dtype=torch.float32, device=device)
-    _check(lib.vf_rotary_table(C.byref(plan), _ptr(table), _stream()))
+    _check(lib.vf_rotary_table(C.byref(plan), _ptr(table), _stream_of(table)))
     return table
 
 
@@ -475,13 +491,15 @@ def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HAL
     slot int32 [rows], pool: one layer's pages (kv_layer)."""
     rows, hq, hd = q.shape
     pages, hkv = _pool(pool, hd, q.dtype)
-    if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous() or not table.is_cuda:
+    positions, half, two = table.shape
+    if two != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or not table.is_cuda:
         _refuse("table: contiguous float32 device tensor [positions, rotary_dim / 2, 2]")
-    args = vf_rotary_args(_dtype(q), hq, hkv, hd, 2 * table.shape[1], pairs, rows, table.shape[0], pages, 0,
-                          _rows("q", q, q.dtype, rows, hq, hd), _rows("k", k, q.dtype, rows, hkv, hd),
-                          _rows("v", v, q.dtype, rows, hkv, hd), _rows("q_out", q_out, q.dtype, rows, hq, hd))
+    dt = q.dtype
+    args = vf_rotary_args(_dtype(q), hq, hkv, hd, 2 * half, pairs, rows, positions, pages, 0,
+                          _rows("q", q, dt, rows, hq, hd), _rows("k", k, dt, rows, hkv, hd),
+                          _rows("v", v, dt, rows, hkv, hd), _rows("q_out", q_out, dt, rows, hq, hd))
     _check(lib.vf_rotary_append(C.byref(args), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                _ints("pos", pos, rows), _ints("slot", slot, rows), q_out.data_ptr(), pool.data_ptr(), _stream()))
+                                _ints("pos", pos, rows), _ints("slot", slot, rows), q_out.data_ptr(), pool.data_ptr(), _stream_of(q)))
 
 
 def _packed_args(q, pool, block_table, out, max_rows, max_keys, scale):
@@ -507,4 +525,4 @@ def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, ma
     args = _packed_args(q, pool, block_table, out, max_rows, max_keys, scale)
     _check(lib.vf_attention_packed(C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
                                    _ints("row_off", row_off, args.n_seqs + 1), _ints("kv_len", kv_len, args.n_seqs),
-                                   out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))
+                                   out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(q)))

@@ -133,8 +133,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
                       wave % (WAVES / 2) * (LPW * 1024);
     const unsigned lds0 = lds_address(smem) + wave * (LPW * 1024);
     const int32_t *table = p.table + (size_t)t.seq * a.table_stride;
-    // ids of 64 pages, one per lane: those from `at` on
-    int ids = 0, ids_at = -64;
+    // ids of 64 pages, one per lane: those from ids_at on
+    int ids_at = p_begin, ids = table[min(p_begin + lane, a.max_pages - 1)];
     auto page_id = [&](int pg) {
         if (pg - ids_at >= 64) {
             ids_at = pg;
@@ -227,37 +227,44 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = mma(v_piece(st, g / 2, g % 2, db), w[g], acc[db]);
     };
-    // the same where some keys are not seen by all items
+    // The same where some keys are not seen by all items.  0 times a value that is not finite is not 0: if a key that only some
+    // items see holds such a value, every row takes the product with its own keys.
     auto products_masked = [&](const unsigned char *st, int t0) {
         const int own = t0 + half * 8, page_last = min(wave_last, t0 + VF_TILE - 1);
-        auto product = [&](auto db, int seen, floatx16 c) {   // keys beyond `seen` are taken as zeros
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                Frag<T> v = v_piece(st, g / 2, g % 2, db);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (own + g * 16 + j > seen) v.v[j] = from_f32<T>(0.f);
-                c = mma(v, w[g], c);
-            }
-            return c;
-        };
         static_for<0, DB>([&](auto db) {
             constexpr int D = db;
-            // 0 times a value that is not finite is not 0: keys beyond all items count as zeros, and if a key that only some
-            // items see holds such a value, every row takes the product with its own keys
-            bool bad = false;
+            // the largest exponents, of two bfloat16 values or one float32 value a word
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 top = {0, 0};
+            Frag<T> v[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const Frag<T> v = v_piece(st, g / 2, g % 2, D);
+                v[g] = v_piece(st, g / 2, g % 2, D);
+                if constexpr (HALVES == 1) {
+                    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+                    const u32x4 x = __builtin_bit_cast(u32x4, v[g]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) bad |= own + g * 16 + j <= page_last && not_finite(to_f32(v.v[j]));
+                    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[j] & 0x7fff7fffu));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) top = __builtin_elementwise_max(top, u16x2{(unsigned short)(__float_as_uint(v[g].v[j]) >> 16 & 0x7fff), 0});
+                }
             }
-            if (!__builtin_amdgcn_ballot_w64(bad)) {
-                acc[D] = product(db, page_last, acc[D]);
+            if (!__builtin_amdgcn_ballot_w64(top[0] >= 0x7f80 || top[1] >= 0x7f80)) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) acc[D] = mma(v[g], w[g], acc[D]);
             } else {
                 floatx16 sum = acc[D];   // of rows that see nothing here
                 for (int seen = max(wave_first, t0); seen <= page_last; ++seen) {
-                    const floatx16 c = product(db, seen, acc[D]);
+                    floatx16 c = acc[D];
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        Frag<T> x = v_piece(st, g / 2, g % 2, D);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (own + g * 16 + j > seen) x.v[j] = from_f32<T>(0.f);
+                        c = mma(x, w[g], c);
+                    }
                     if (min(last_key, t0 + VF_TILE - 1) == seen) sum = c;
                 }
                 acc[D] = sum;
@@ -265,13 +272,26 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             __builtin_amdgcn_sched_barrier(0);   // one block's values in registers at a time
         });
     };
+    // Memory behind the last key may hold anything: its values count as zeros.
+    auto clear_behind = [&](unsigned char *st, int keys) {   // keys: of the page that are there
+        for (int u = threadIdx.x; u < UNITS / 2 * 64; u += WAVES * 64) {
+            const int piece = HALVES == 1 ? u : (u >> 7 << 6) + (u & 63), e0 = HALVES == 1 ? 0 : (u >> 6 & 1) * 4;
+            const int there = keys - (piece / (DB * 128) * 32 + (piece >> 4 & 3) * 8) - e0;   // of this unit's 16 / sizeof(T) elements
+            if (there >= 16 / (int)sizeof(T)) continue;
+            T *x = reinterpret_cast<T *>(st + UNITS / 2 * 1024 + u * 16);
+#pragma unroll
+            for (int j = 0; j < 16 / (int)sizeof(T); ++j)
+                if (j >= there) x[j] = from_f32<T>(0.f);
+        }
+    };
     // Steps: page i's weights and products, and the scores of page i + 1, which do not wait for them.
     const int n = p_end - p_begin;
     if (n > 0) {
         // pages that all items see whole, up to the first that is not in the pool
         int n_full = max(0, min(n, (min(first_pos + t.item0 / group, cap - 1) + 1) / VF_TILE - p_begin));
         for (int i0 = 0; i0 < n_full; i0 += 64) {
-            const unsigned long long missing = __builtin_amdgcn_ballot_w64((unsigned)table[p_begin + min(i0 + lane, n_full - 1)] >= (unsigned)a.pool_pages);
+            const int id = i0 ? table[p_begin + min(i0 + lane, n_full - 1)] : ids;
+            const unsigned long long missing = __builtin_amdgcn_ballot_w64(i0 + lane < n_full && (unsigned)id >= (unsigned)a.pool_pages);
             if (missing) n_full = min(n_full, i0 + __builtin_ctzll(missing));
         }
         auto k_page = [&](int i) { return smem + ((p_begin + i) & 1) * (UNITS * 1024); };
@@ -280,12 +300,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             lds_sync();
             issue(i + 1);
         };
+        auto tail = [&](int i) {   // behind a step past n_full
+            const int keys = cap - (p_begin + i) * VF_TILE;
+            if (keys < VF_TILE) {
+                clear_behind(smem + ((p_begin + i) & 1) * (UNITS * 1024), keys);
+                lds_sync();
+            }
+        };
         issue(-1);
         vm_wait<0>();
         lds_sync();
         issue(0);
         if (!has_items) {
-            for (int i = 0; i < n; ++i) step(i);
+            for (int i = 0; i < n; ++i) {
+                step(i);
+                if (i >= n_full) tail(i);
+            }
         } else {
             int i = 0;
             if (n_full > 0) {
@@ -320,6 +350,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
                 Scores sc;
                 if (mine) sc = scores(k_page(i));
                 step(i);
+                tail(i);
                 if (!mine) continue;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
@@ -588,17 +619,37 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
     const long long idx = (long long)blockIdx.x * (256 / TH) + threadIdx.x / TH;
     const int row = (int)(idx / a.n_q_heads), head = (int)(idx % a.n_q_heads), d0 = threadIdx.x % TH * 4;
     if (row >= a.total_rows || row < p.row_off[0] || row >= p.row_off[a.n_seqs]) return;
-    const int used = p.used[row];
     const float *rec = p.records + ((size_t)row * a.n_q_heads + head) * p.parts * REC;
     float M = -1e30f, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < used; ++i, rec += REC) {
-        const float2 ml = *reinterpret_cast<const float2 *>(rec);
-        const floatx4 v = *reinterpret_cast<const floatx4 *>(rec + REC_HEAD + d0);
-        const float m = fmaxf(M, ml.x), keep = __builtin_amdgcn_exp2f(M - m), add = __builtin_amdgcn_exp2f(ml.x - m);
-        L = L * keep + ml.y * add;
-        acc = acc * keep + v * add;
+    // NR records are asked for together, with the number of those that count
+    constexpr int NR = 8;
+    int used = p.parts;
+    for (int i0 = 0; i0 < used; i0 += NR) {
+        float2 ml[NR];
+        floatx4 v[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const float *r = rec + (size_t)min(i0 + i, p.parts - 1) * REC;
+            ml[i] = *reinterpret_cast<const float2 *>(r);
+            v[i] = *reinterpret_cast<const floatx4 *>(r + REC_HEAD + d0);
+        }
+        used = min(p.parts, p.used[row]);
+        float m = M;
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+            if (i0 + i < used) m = fmaxf(m, ml[i].x);
+        const float keep = __builtin_amdgcn_exp2f(M - m);
+        L *= keep;
+        acc *= keep;
         M = m;
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+            if (i0 + i < used) {
+                const float add = __builtin_amdgcn_exp2f(ml[i].x - m);
+                L += ml[i].y * add;
+                acc += v[i] * add;
+            }
     }
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     typedef T four __attribute__((ext_vector_type(4)));

@@ -14,12 +14,24 @@
 
 namespace {
 
+// Division by a number the host knows: a multiplication that is at most one too high, put right.
+struct Divisor {
+    unsigned d, m;
+    __device__ __forceinline__ int operator()(int n) const {   // n / d, n >= 0
+        if (d == 1) return n;
+        const unsigned q = __umulhi((unsigned)n, m);
+        return (int)(q - (q * d > (unsigned)n));
+    }
+};
+inline Divisor divisor(unsigned d) { return {d, d > 1 ? (unsigned)((1ull << 32) / d + 1) : 0}; }
+
 struct PackedAttn {
     vf_packed_args a;
     const void *q, *kv;
     const int32_t *table, *row_off, *kv_len;
     void *out;
     int32_t group, tiles, parts, part_pages;   // tiles: items tiles of all sequences, at most
+    Divisor by_group, by_heads, by_parts, by_q_heads;
     float scale_log2e;
     float *records;                            // [row][head][part][REC_HEAD + head_dim], parts > 1
     int32_t *used;                             // [row]: parts with a record
@@ -99,22 +111,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     extern __shared__ __align__(1024) unsigned char smem[];
     const vf_packed_args &a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
-    const int part = rest % p.parts;
-    const Tile t = find_tile<BM>(p, p.tiles - 1 - rest / p.parts);
+    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, place = p.by_parts(rest), part = rest - place * p.parts;
+    const Tile t = find_tile<BM>(p, p.tiles - 1 - place);
     if (t.rows <= 0) return;
     const int group = p.group, n_items = t.rows * group, cap = min(t.kv_len, a.max_pages * VF_TILE);
     const int first_pos = t.kv_len - t.rows;                    // position of row 0
     const int wave0 = t.item0 + wave * 32, item = min(n_items - 1, wave0 + col);
-    const int row = t.row0 + item / group, head = kvh * group + item % group;
-    const int last_key = min(first_pos + item / group, cap - 1);
-    const int tile_last = min(first_pos + min(n_items - 1, t.item0 + BM - 1) / group, cap - 1);
+    const int item_row = p.by_group(item), item_head = item - item_row * group, row = t.row0 + item_row, head = kvh * group + item_head;
+    const int last_key = min(first_pos + item_row, cap - 1);
+    const int tile_last = min(first_pos + p.by_group(min(n_items - 1, t.item0 + BM - 1)), cap - 1);
+    const int tile_first = min(first_pos + p.by_group(t.item0), cap - 1);
     const bool has_items = wave0 < n_items;   // a wavefront without items still brings its share of the pages
-    const int wave_last = has_items ? min(first_pos + min(n_items - 1, wave0 + 31) / group, cap - 1) : -1;
-    const int wave_first = min(first_pos + min(n_items - 1, wave0) / group, cap - 1);
+    const int wave_last = has_items ? min(first_pos + p.by_group(min(n_items - 1, wave0 + 31)), cap - 1) : -1;
+    const int wave_first = min(first_pos + p.by_group(min(n_items - 1, wave0)), cap - 1);
     const int pages = tile_last < 0 ? 0 : tile_last / VF_TILE + 1;
     const int p_begin = part * p.part_pages, p_end = part == p.parts - 1 ? pages : min(pages, p_begin + p.part_pages);
-    if (p.parts > 1 && part == 0 && kvh == 0 && wave0 + col < n_items && half == 0 && item % group == 0)
+    if (p.parts > 1 && part == 0 && kvh == 0 && wave0 + col < n_items && half == 0 && item_head == 0)
         p.used[row] = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
     if (p_begin >= p_end && part > 0) return;
 
@@ -288,7 +300,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     const int n = p_end - p_begin;
     if (n > 0) {
         // pages that all items see whole, up to the first that is not in the pool
-        int n_full = max(0, min(n, (min(first_pos + t.item0 / group, cap - 1) + 1) / VF_TILE - p_begin));
+        int n_full = max(0, min(n, (tile_first + 1) / VF_TILE - p_begin));
         for (int i0 = 0; i0 < n_full; i0 += 64) {
             const int id = i0 ? table[p_begin + min(i0 + lane, n_full - 1)] : ids;
             const unsigned long long missing = __builtin_amdgcn_ballot_w64(i0 + lane < n_full && (unsigned)id >= (unsigned)a.pool_pages);
@@ -416,7 +428,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
     float *maxima = sums + WAVES * BM * OUT, *totals = maxima + WAVES * BM;
     const vf_packed_args &a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4, l15 = lane & 15;
-    const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % p.parts, seq = rest / p.parts;
+    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, seq = p.by_parts(rest), part = rest - seq * p.parts;
     const int p_first = part * p.part_pages;
     const int32_t *table = p.table + (size_t)seq * a.table_stride;
     int ids = table[min(p_first + lane, a.max_pages - 1)];   // asked for with the lengths
@@ -425,19 +437,20 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
     const int group = p.group, n_items = rows * group, cap = min(kv_len, a.max_pages * VF_TILE), first_pos = kv_len - rows;
     const size_t page_bytes = (size_t)2 * a.n_kv_heads * VF_TILE * HD * sizeof(T), head_bytes = (size_t)VF_TILE * HD * sizeof(T);
     for (int item0 = 0; item0 < n_items; item0 += BM) {
-        const int last = min(first_pos + min(n_items - 1, item0 + BM - 1) / group, cap - 1);   // last key that an item sees
+        const int last = min(first_pos + p.by_group(min(n_items - 1, item0 + BM - 1)), cap - 1);   // last key that an item sees
         const int pages = last < 0 ? 0 : last / VF_TILE + 1, parts = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
         const int p_end = part == p.parts - 1 ? pages : min(pages, p_first + p.part_pages);
         if (p.parts > 1 && part == 0 && kvh == 0 && threadIdx.x < BM && item0 + (int)threadIdx.x < n_items)
-            p.used[row0 + (item0 + threadIdx.x) / group] = parts;
+            p.used[row0 + p.by_group(item0 + threadIdx.x)] = parts;
         if (p_first >= p_end && part > 0) continue;
         int last_key[NB];
         Frag<T> qf[NB][KD];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int item = min(n_items - 1, item0 + nb * 16 + l15);
-            last_key[nb] = min(first_pos + item / group, cap - 1);
-            const T *q = (const T *)p.q + (row0 + item / group) * a.q_stride + (kvh * group + item % group) * HD + g4 * 8;
+            const int item_row = p.by_group(item);
+            last_key[nb] = min(first_pos + item_row, cap - 1);
+            const T *q = (const T *)p.q + (row0 + item_row) * a.q_stride + (kvh * group + item - item_row * group) * HD + g4 * 8;
 #pragma unroll
             for (int kd = 0; kd < KD; ++kd) qf[nb][kd] = load_frag<T>((const char *)(q + kd * 32));
         }
@@ -451,7 +464,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
             for (int db = 0; db < DB; ++db) acc[nb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
         // keys 32 i .. + 31, i = 2 p_first + wave, + WAVES ..
-        const int first_all = min(first_pos + item0 / group, cap - 1);   // last key that all items see
+        const int first_all = min(first_pos + p.by_group(item0), cap - 1);   // last key that all items see
         const int i_end = min(2 * p_end, last / 32 + 1);
         int ids_at = p_first;
         Frag<T> k[2 * KD], v[DB];   // a tile's keys are asked for when those before have been multiplied, its values likewise
@@ -594,7 +607,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] += sums[(w * BM + it) * OUT + d0 + e] * f;
             }
-            const int row = row0 + item / group, head = kvh * group + item % group;
+            const int item_row = p.by_group(item), row = row0 + item_row, head = kvh * group + item - item_row * group;
             if (p.parts > 1) {
                 float *rec = p.records + (((size_t)row * a.n_q_heads + head) * p.parts + part) * (REC_HEAD + HD);
                 if (d0 == 0) *reinterpret_cast<float2 *>(rec) = float2{M, L};
@@ -616,8 +629,8 @@ template <typename T, int HD>
 __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
     constexpr int REC = HD + REC_HEAD, TH = HD / 4;
     const vf_packed_args &a = p.a;
-    const long long idx = (long long)blockIdx.x * (256 / TH) + threadIdx.x / TH;
-    const int row = (int)(idx / a.n_q_heads), head = (int)(idx % a.n_q_heads), d0 = threadIdx.x % TH * 4;
+    const int idx = blockIdx.x * (256 / TH) + threadIdx.x / TH;
+    const int row = p.by_q_heads(idx), head = idx - row * a.n_q_heads, d0 = threadIdx.x % TH * 4;
     if (row >= a.total_rows || row < p.row_off[0] || row >= p.row_off[a.n_seqs]) return;
     const float *rec = p.records + ((size_t)row * a.n_q_heads + head) * p.parts * REC;
     float M = -1e30f, L = 0.f;
@@ -769,6 +782,10 @@ int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const voi
     p.parts = plan.parts;
     p.part_pages = plan.part_pages;
     p.scale_log2e = (p.a.scale == 0.f ? 1.0f / sqrtf((float)p.a.head_dim) : p.a.scale) * 1.4426950408889634f;
+    p.by_group = divisor(p.group);
+    p.by_heads = divisor(p.a.n_kv_heads);
+    p.by_parts = divisor(plan.parts);
+    p.by_q_heads = divisor(p.a.n_q_heads);
     p.records = (float *)workspace_dev;
     p.used = (int32_t *)((char *)workspace_dev + plan.bytes - (size_t)p.a.total_rows * sizeof(int32_t));
     const auto go = p.a.dtype == VF_BF16 ? (p.a.head_dim == 128 ? launch<bf16_t, 128> : launch<bf16_t, 64>)

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "lds_stream.h"
 #include "vf_internal.h"
 
 namespace {
@@ -169,56 +170,168 @@ template <typename T> __device__ __forceinline__ void turn_unit(Eight<T> &lo, Ei
     for (int i = 0; i < 8; ++i) { lo.v[i] = from_f32<T>(y[i]); hi.v[i] = from_f32<T>(y[8 + i]); }
 }
 
-// One thread: one unit of one head of a row of q or k, or eight elements of a row of v.
+// What bounds it is memory, and how the cache is written.  A page keeps four consecutive tokens' eight-element pieces of K next
+// to one another and those of tokens 8 further behind them, and eight consecutive tokens of one feature of V.  So there are
+// three kinds of workgroups: 16 rows of some heads of q, lanes along the row; the same of k, lanes along the tokens; and 64 rows
+// of one head of v, which go through LDS to be written as pieces of eight tokens; v, with the longest way, comes first.  Workgroups of
+// k and v whose rows are neighbours run on one die, whose L2 joins what they write to one line.  A thread of q and k keeps its row's angles
+// over BATCH heads and asks for all their pieces before it turns the first.
+constexpr int ROTARY_ROWS = 16, ROTARY_V_ROWS = 64, BATCH = 4;
+
+struct RotaryGrid { int32_t heads, v, k, v_rows, v_single; };   // heads a workgroup of q or k; workgroups of v, of k; rows a workgroup of v; each by itself
+
 template <typename T, int HD, bool HALF>
-__global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, const T *q, const T *__restrict__ k,
+__device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const T *src, int64_t src_stride, const float2 *table, const int32_t *pos,
+                                            const int32_t *slot, T *out, bool is_k, int row, int ui, int h, int h1) {
+    constexpr int SIDE = 256 / (ROTARY_ROWS * (HD / 16));   // heads side by side
+    if (row >= a.total_rows) return;
+    const Unit u = unit_of(ui, a.rotary_dim, HALF);
+    const int p = pos[row], s = is_k ? slot[row] : 0;
+    const bool at = p >= 0 && p < a.max_positions;
+    if (is_k && (!at || s < 0 || s >= a.pool_pages * VF_TILE)) return;
+    float2 angle[8];
+    if (u.turns) {
+        const float4 *from = reinterpret_cast<const float4 *>(table + (size_t)(at ? p : 0) * (a.rotary_dim / 2) + ui * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 x = from[i];
+            angle[2 * i] = make_float2(x.x, x.y);
+            angle[2 * i + 1] = make_float2(x.z, x.w);
+        }
+    }
+    src += row * src_stride;
+    const int per_head = is_k ? VF_TILE * HD : HD;
+    const size_t to_lo = is_k ? kv_k_index(0, 0, s / VF_TILE, a.n_kv_heads, 0, s % VF_TILE, u.lo, HD) : (size_t)(row * a.q_out_stride) + u.lo;
+    const size_t to_hi = is_k ? kv_k_index(0, 0, s / VF_TILE, a.n_kv_heads, 0, s % VF_TILE, u.hi, HD) : (size_t)(row * a.q_out_stride) + u.hi;
+    for (; h < h1; h += BATCH * SIDE) {
+        Eight<T> lo[BATCH], hi[BATCH];
+        auto load = [&](int i) {
+            const T *x = src + (h + i * SIDE) * HD;
+            lo[i] = eight(x + u.lo);
+            hi[i] = eight(x + u.hi);
+        };
+        if (h + (BATCH - 1) * SIDE < h1) {   // (loads with conditions of their own would be waited for all together)
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) load(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (h + i * SIDE < h1) load(i);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int head = h + i * SIDE;
+            if (head >= h1) break;
+            if (u.turns) turn_unit(lo[i], hi[i], angle, HALF);
+            if (!at) lo[i] = hi[i] = Eight<T>{};
+            put_eight(out + to_lo + (size_t)head * per_head, lo[i]);
+            put_eight(out + to_hi + (size_t)head * per_head, hi[i]);
+        }
+    }
+}
+
+template <typename T, int HD, bool HALF>
+__global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, RotaryGrid g, const T *q, const T *__restrict__ k,
                                                             const T *__restrict__ v, const float2 *__restrict__ table,
                                                             const int32_t *__restrict__ pos, const int32_t *__restrict__ slot,
                                                             T *q_out, T *__restrict__ kv) {
-    const int hq = a.n_q_heads, hkv = a.n_kv_heads, per_row = (hq + hkv) * (HD / 16) + hkv * (HD / 8);
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(id / per_row), i = (int)(id % per_row);
-    if (row >= a.total_rows) return;
-    const int p = pos[row], s = slot[row];
-    const bool at = p >= 0 && p < a.max_positions, stored = at && s >= 0 && s / VF_TILE < a.pool_pages;
-    const int page = s / VF_TILE, tin = s % VF_TILE;
-    if (i < (hq + hkv) * (HD / 16)) {
-        const int head = i / (HD / 16);
-        const Unit u = unit_of(i % (HD / 16), a.rotary_dim, HALF);
-        const bool is_q = head < hq;
-        if (!is_q && !stored) return;
-        const T *src = is_q ? q + row * a.q_stride + head * HD : k + row * a.k_stride + (head - hq) * HD;
-        Eight<T> lo = eight(src + u.lo), hi = eight(src + u.hi);
-        if (at && u.turns) turn_unit(lo, hi, table + (size_t)p * (a.rotary_dim / 2) + i % (HD / 16) * 8, HALF);
-        if (is_q) {
-            if (!at) lo = hi = Eight<T>{};
-            T *dst = q_out + row * a.q_out_stride + head * HD;
-            put_eight(dst + u.lo, lo);
-            put_eight(dst + u.hi, hi);
-        } else {
-            put_eight(kv + kv_k_index(0, 0, page, hkv, head - hq, tin, u.lo, HD), lo);
-            put_eight(kv + kv_k_index(0, 0, page, hkv, head - hq, tin, u.hi, HD), hi);
-        }
-    } else if (stored) {
-        const int j = i - (hq + hkv) * (HD / 16), head = j / (HD / 8), d0 = j % (HD / 8) * 8;
-        const Eight<T> x = eight(v + row * a.v_stride + head * HD + d0);
+    constexpr int UNITS = HD / 16, SIDE = 256 / (ROTARY_ROWS * UNITS);
+    const int hq = a.n_q_heads, hkv = a.n_kv_heads, tid = threadIdx.x;
+    int w = blockIdx.x;
+    if (w >= g.k + g.v) {
+        w -= g.k + g.v;
+        const int per = (hq + g.heads - 1) / g.heads, h0 = w % per * g.heads;
+        rotate_rows<T, HD, HALF>(a, q, a.q_stride, table, pos, slot, q_out, false, w / per * ROTARY_ROWS + tid / (UNITS * SIDE), tid % UNITS,
+                                 h0 + tid / UNITS % SIDE, min(h0 + g.heads, hq));
+        return;
+    }
+    if (w >= g.v) {
+        w = die_order(w - g.v, g.k);
+        const int per = (hkv + g.heads - 1) / g.heads, h0 = w % per * g.heads;
+        rotate_rows<T, HD, HALF>(a, k, a.k_stride, table, pos, slot, kv, true, w / per * ROTARY_ROWS + tid % ROTARY_ROWS, tid / ROTARY_ROWS % UNITS,
+                                 h0 + tid / (ROTARY_ROWS * UNITS), min(h0 + g.heads, hkv));
+        return;
+    }
+    w = die_order(w, g.v);
+    const int head = w % hkv, r0 = w / hkv * g.v_rows, n_slots = a.pool_pages * VF_TILE;
+    v += head * HD;
+    kv += (size_t)(hkv + head) * VF_TILE * HD;
+    const size_t page_size = (size_t)2 * hkv * VF_TILE * HD;
+    auto slot_of = [&](int row) {   // -1: not stored
+        if (row < 0 || row >= a.total_rows) return -1;
+        const int p = pos[row], s = slot[row];
+        return p >= 0 && p < a.max_positions && s >= 0 && s < n_slots ? s : -1;
+    };
+    auto place = [&](int s, int d) { return (size_t)(s / VF_TILE) * page_size + kv_v_index(0, 0, 0, 0, 0, s % VF_TILE, d, HD); };
+    if (g.v_single) {   // few rows
+        const int row = r0 + tid / (HD / 8), d0 = tid % (HD / 8) * 8;
+        if (tid / (HD / 8) >= g.v_rows || row >= a.total_rows) return;
+        const Eight<T> x = eight(v + row * a.v_stride + d0);
+        const int s = slot_of(row);
+        if (s < 0) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) kv[kv_v_index(0, 0, page, hkv, head, tin, d0 + e, HD)] = x.v[e];
+        for (int e = 0; e < 8; ++e) kv[place(s, d0) + e * 8] = x.v[e];
+        return;
+    }
+    // Rows r0 - 7 .. r0 + v_rows + 6.  Eight rows with eight slots in a row from a multiple of eight on are a run; it belongs to
+    // the workgroup that has its first row.
+    constexpr int PAD = HD + 16 / (int)sizeof(T);
+    __shared__ __align__(16) T rows[ROTARY_V_ROWS + 7][PAD];
+    __shared__ int slots[ROTARY_V_ROWS + 14];
+    __shared__ int firsts[ROTARY_V_ROWS], alone[ROTARY_V_ROWS], n_firsts, n_alone;
+    if (tid == 0) n_firsts = n_alone = 0;
+    if (tid < g.v_rows + 14) slots[tid] = slot_of(r0 - 7 + tid);
+    constexpr int MOST = ((ROTARY_V_ROWS + 7) * (HD / 8) + 255) / 256;
+    const int pieces = (g.v_rows + 7) * (HD / 8);
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        const int j = tid + i * 256, row = min(r0 + j / (HD / 8), a.total_rows - 1);
+        if (j < pieces) *reinterpret_cast<Eight<T> *>(&rows[j / (HD / 8)][j % (HD / 8) * 8]) = eight(v + row * a.v_stride + j % (HD / 8) * 8);
+    }
+    __syncthreads();
+    if (tid < g.v_rows && slots[tid + 7] >= 0) {
+        const int s = slots[tid + 7], first = tid + 7 - s % 8;
+        bool run = first >= 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) run = run && slots[max(first, 0) + i] == s - s % 8 + i;
+        if (!run) alone[atomicAdd(&n_alone, 1)] = tid;
+        else if (s % 8 == 0) firsts[atomicAdd(&n_firsts, 1)] = tid;
+    }
+    __syncthreads();
+    for (int j = tid; j < n_firsts * HD; j += 256) {
+        const int r = firsts[j / HD], d = j % HD;
+        Eight<T> x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.v[i] = rows[r + i][d];
+        put_eight(kv + place(slots[r + 7], d), x);
+    }
+    for (int j = tid; j < n_alone * HD; j += 256) {
+        const int r = alone[j / HD], d = j % HD;
+        kv[place(slots[r + 7], d)] = rows[r][d];
     }
 }
 
 template <typename T, int HD>
 int launch_rotary(const vf_rotary_args &a, const void *q, const void *k, const void *v, const float *table, const int32_t *pos,
-                   const int32_t *slot, void *q_out, void *kv, hipStream_t st) {
-    const long long threads = (long long)a.total_rows * ((a.n_q_heads + a.n_kv_heads) * (HD / 16) + a.n_kv_heads * (HD / 8));
-    if (threads >= 0xffffff00LL) return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: %d rows of %d heads in one call", a.total_rows, a.n_q_heads + 2 * a.n_kv_heads);
-    const dim3 grid((unsigned)((threads + 255) / 256));
-    if (a.pairs == VF_ROTARY_HALF)
-        hipLaunchKernelGGL((rotary_append_kernel<T, HD, true>), grid, dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v,
-                           (const float2 *)table, pos, slot, (T *)q_out, (T *)kv);
-    else
-        hipLaunchKernelGGL((rotary_append_kernel<T, HD, false>), grid, dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v,
-                           (const float2 *)table, pos, slot, (T *)q_out, (T *)kv);
+                  const int32_t *slot, void *q_out, void *kv, hipStream_t st) {
+    const int tiles = (a.total_rows + ROTARY_ROWS - 1) / ROTARY_ROWS, side = 256 / (ROTARY_ROWS * (HD / 16));
+    RotaryGrid g;
+    // as many heads a workgroup as leave the chip about eight workgroups a compute unit, at most BATCH for a thread
+    g.heads = std::min((int)std::max(1ll, (long long)tiles * (a.n_q_heads + a.n_kv_heads) / (2048 * side)), BATCH) * side;
+    // v: up to 128 K elements each row by itself (777 rows of two heads of 64: 3.0 us a call for 3.4), else tiles of 64 rows, or of
+    // 32 or 16 where that leaves fewer than 100 workgroups (512 rows of eight heads of 128: 5.7, 5.1, 4.8; 2000 of two: 7.2, 6.4, 6.7)
+    g.v_single = (long long)a.total_rows * a.n_kv_heads * HD <= 128 * 1024;
+    g.v_rows = g.v_single ? 256 / (HD / 8) : ROTARY_V_ROWS;
+    while (!g.v_single && g.v_rows > 16 && (long long)((a.total_rows + g.v_rows - 1) / g.v_rows) * a.n_kv_heads < 100) g.v_rows /= 2;
+    const long long n_q = (long long)tiles * ((a.n_q_heads + g.heads - 1) / g.heads), n_k = (long long)tiles * ((a.n_kv_heads + g.heads - 1) / g.heads);
+    const long long n_v = (long long)((a.total_rows + g.v_rows - 1) / g.v_rows) * a.n_kv_heads, blocks = n_q + n_k + n_v;
+    if (blocks > 0xffffff)
+        return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: %d rows of %d heads in one call", a.total_rows, a.n_q_heads + 2 * a.n_kv_heads);
+    g.v = (int32_t)n_v;
+    g.k = (int32_t)n_k;
+    const auto kernel = a.pairs == VF_ROTARY_HALF ? rotary_append_kernel<T, HD, true> : rotary_append_kernel<T, HD, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, g, (const T *)q, (const T *)k, (const T *)v, (const float2 *)table,
+                       pos, slot, (T *)q_out, (T *)kv);
     VF_LAUNCH_CHECK("rotary_append");
     return VF_OK;
 }
@@ -290,7 +403,7 @@ int vf_rotary_append(const vf_rotary_args *args, const void *q_dev, const void *
                        (long long)a.k_stride, (long long)a.v_stride, (long long)a.q_out_stride);
     if (q_out_dev == q_dev && a.q_out_stride != a.q_stride) return vf_fail(VF_ERR_ARG, "vf_rotary_append: q in place with another stride");
     if (((a.q_stride | a.k_stride | a.v_stride | a.q_out_stride) * es | (int64_t)(uintptr_t)q_dev | (int64_t)(uintptr_t)k_dev |
-         (int64_t)(uintptr_t)v_dev | (int64_t)(uintptr_t)q_out_dev | (int64_t)(uintptr_t)kv_layer_dev) & 15 || (uintptr_t)table_dev & 7)
+         (int64_t)(uintptr_t)v_dev | (int64_t)(uintptr_t)q_out_dev | (int64_t)(uintptr_t)kv_layer_dev) & 15 || (uintptr_t)table_dev & 15)
         return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: addresses and strides are multiples of 16 bytes");
     hipStream_t st = (hipStream_t)stream;
     const auto launch = a.dtype == VF_BF16 ? (a.head_dim == 128 ? launch_rotary<bf16_t, 128> : launch_rotary<bf16_t, 64>)

@@ -31,7 +31,7 @@ struct PackedAttn {
     const int32_t *table, *row_off, *kv_len;
     void *out;
     int32_t group, tiles, parts, part_pages;   // tiles: items tiles of all sequences, at most
-    Divisor by_group, by_heads, by_parts, by_q_heads;
+    Divisor by_group, by_heads, by_tiles, by_q_heads;
     float scale_log2e;
     float *records;                            // [row][head][part][REC_HEAD + head_dim], parts > 1
     int32_t *used;                             // [row]: parts with a record
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     extern __shared__ __align__(1024) unsigned char smem[];
     const vf_packed_args &a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
-    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, place = p.by_parts(rest), part = rest - place * p.parts;
+    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, part = p.by_tiles(rest), place = rest - part * p.tiles;
     const Tile t = find_tile<BM>(p, p.tiles - 1 - place);
     if (t.rows <= 0) return;
     const int group = p.group, n_items = t.rows * group, cap = min(t.kv_len, a.max_pages * VF_TILE);
@@ -423,12 +423,12 @@ template <typename T> __device__ __forceinline__ Frag<T> load_frag(const char *a
 
 template <typename T, int HD, int WAVES, int NB>
 __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kernel(PackedAttn p) {
-    constexpr int KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = 16 * NB, OUT = HD + 1;   // FRAG: bytes; OUT: stride of a sum in LDS
+    constexpr int KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = 16 * NB, OUT = HD + 4;   // FRAG: bytes; OUT: stride of a sum in LDS
     extern __shared__ __align__(16) float sums[];   // [WAVES][BM][OUT], then maxima and sums of weights
     float *maxima = sums + WAVES * BM * OUT, *totals = maxima + WAVES * BM;
     const vf_packed_args &a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4, l15 = lane & 15;
-    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, seq = p.by_parts(rest), part = rest - seq * p.parts;
+    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, part = p.by_tiles(rest), seq = rest - part * p.tiles;
     const int p_first = part * p.part_pages;
     const int32_t *table = p.table + (size_t)seq * a.table_stride;
     int ids = table[min(p_first + lane, a.max_pages - 1)];   // asked for with the lengths
@@ -588,9 +588,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
             const int at = wave * BM + nb * 16 + l15;
             if (g4 == 0) { maxima[at] = m_run[nb]; totals[at] = l; }
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sums[at * OUT + db * 16 + g4 * 4 + e] = acc[nb][db][e];
+            for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4 *>(&sums[at * OUT + db * 16 + g4 * 4]) = acc[nb][db];
         }
         __syncthreads();
         for (int j = threadIdx.x; j < BM * (HD / 4); j += WAVES * 64) {
@@ -604,8 +602,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
             for (int w = 0; w < WAVES; ++w) {
                 const float f = __builtin_amdgcn_exp2f(maxima[w * BM + it] - M);
                 L += totals[w * BM + it] * f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += sums[(w * BM + it) * OUT + d0 + e] * f;
+                o += *reinterpret_cast<const floatx4 *>(&sums[(w * BM + it) * OUT + d0]) * f;
             }
             const int item_row = p.by_group(item), row = row0 + item_row, head = kvh * group + item - item_row * group;
             if (p.parts > 1) {
@@ -631,7 +628,8 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
     const vf_packed_args &a = p.a;
     const int idx = blockIdx.x * (256 / TH) + threadIdx.x / TH;
     const int row = p.by_q_heads(idx), head = idx - row * a.n_q_heads, d0 = threadIdx.x % TH * 4;
-    if (row >= a.total_rows || row < p.row_off[0] || row >= p.row_off[a.n_seqs]) return;
+    if (row >= a.total_rows) return;
+    const bool inside = row >= p.row_off[0] && row < p.row_off[a.n_seqs];
     const float *rec = p.records + ((size_t)row * a.n_q_heads + head) * p.parts * REC;
     float M = -1e30f, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -664,6 +662,7 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
                 acc += v[i] * add;
             }
     }
+    if (!inside) return;
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     typedef T four __attribute__((ext_vector_type(4)));
     four x;
@@ -723,6 +722,9 @@ Plan make_plan(const vf_packed_args &a) {
     return r;
 }
 
+// Workgroups in the order of their numbers: the first parts of all tiles (those that exist for all), then the second .. A die takes every
+// eighth workgroup: with the parts of a tile next to one another some dies had the full ones and some the rest
+// (a prompt of 4096 tokens at 0.5B in two parts 70 us).
 template <typename F> int start(F kernel, long long blocks, int threads, int lds, const PackedAttn &p, hipStream_t st) {
     if (blocks > 0x7fffff) return vf_fail(VF_ERR_UNSUPPORTED, "vf_attention_packed: %lld workgroups", blocks);
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, st, p);
@@ -730,10 +732,10 @@ template <typename F> int start(F kernel, long long blocks, int threads, int lds
     return VF_OK;
 }
 template <typename T, int HD, int NB> int launch_few(const PackedAttn &p, hipStream_t st) {
-    constexpr int LDS = FEW_WAVES * 16 * NB * (HD + 3) * 4;
+    constexpr int LDS = FEW_WAVES * 16 * NB * (HD + 6) * 4;
     static const hipError_t set = hipFuncSetAttribute((const void *)attention_few_kernel<T, HD, FEW_WAVES, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     VF_HIP(set);
-    return start(attention_few_kernel<T, HD, FEW_WAVES, NB>, (long long)p.a.n_seqs * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
+    return start(attention_few_kernel<T, HD, FEW_WAVES, NB>, (long long)p.tiles * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
 }
 template <typename T, int HD> int launch_tiles(const PackedAttn &p, hipStream_t st) {
     constexpr int LDS = 2 * HD / 4 * 1024 * (int)sizeof(T) / 2;
@@ -784,7 +786,7 @@ int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const voi
     p.scale_log2e = (p.a.scale == 0.f ? 1.0f / sqrtf((float)p.a.head_dim) : p.a.scale) * 1.4426950408889634f;
     p.by_group = divisor(p.group);
     p.by_heads = divisor(p.a.n_kv_heads);
-    p.by_parts = divisor(plan.parts);
+    p.by_tiles = divisor(plan.tiles);
     p.by_q_heads = divisor(p.a.n_q_heads);
     p.records = (float *)workspace_dev;
     p.used = (int32_t *)((char *)workspace_dev + plan.bytes - (size_t)p.a.total_rows * sizeof(int32_t));

@@ -206,12 +206,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
         return sc;
     };
     Frag<T> w[4];
-    auto weights = [&](const Scores &sc) {
+    // The weights' common factor follows the maximum with slack: they stay below 2^8, and the sums are rescaled in few pages.
+    auto follow = [&](const Scores &sc) {
         float mx = sc.t[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc.t[i >> 4][i & 15]);
         mx = halves_max(mx) * p.scale_log2e;
-        // The weights' common factor follows the maximum with slack: they stay below 2^8, and the sums are rescaled in few pages.
         if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {
             const float m_new = fmaxf(m_run, mx), keep = __builtin_amdgcn_exp2f(m_run - m_new);
             l_run *= keep;
@@ -219,6 +219,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             for (int db = 0; db < DB; ++db) acc[db] *= keep;
             m_run = m_new;
         }
+    };
+    auto weights = [&](const Scores &sc) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             const float x = __builtin_amdgcn_exp2f(fmaf(sc.t[i >> 4][i & 15], p.scale_log2e, -m_run));
@@ -320,9 +322,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             }
         };
         issue(-1);
-        vm_wait<0>();
-        lds_sync();
         issue(0);
+        vm_wait<LPW>();
+        lds_sync();
         if (!has_items) {
             for (int i = 0; i < n; ++i) {
                 step(i);
@@ -332,6 +334,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             int i = 0;
             if (n_full > 0) {
                 Scores even = scores(k_page(0)), odd;
+                follow(even);
                 auto last = [&](const Scores &sc) {
                     step(i);
                     weights(sc);
@@ -343,6 +346,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
                     ahead = scores(k_page(i + 1));
                     weights(sc);
                     products(k_page(i));
+                    follow(ahead);
                     ++i;
                 };
                 while (i + 2 < n_full) {
@@ -367,6 +371,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
                     if (t0 + half * 8 + (j >> 3) * 16 + (j & 7) > last_key) sc.t[j >> 4][j & 15] = -INFINITY;
+                follow(sc);
                 weights(sc);
                 products_masked(k_page(i), t0);
             }
@@ -633,19 +638,19 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
     const float *rec = p.records + ((size_t)row * a.n_q_heads + head) * p.parts * REC;
     float M = -1e30f, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    // NR records are asked for together, with the number of those that count
+    // NR records are asked for together; how many there are is read first (asked for with all of a row's records, which spares
+    // a round trip, many rows took up to a quarter longer for records that are not there, and few no less)
     constexpr int NR = 8;
-    int used = p.parts;
+    const int used = min(p.parts, p.used[row]);
     for (int i0 = 0; i0 < used; i0 += NR) {
         float2 ml[NR];
         floatx4 v[NR];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const float *r = rec + (size_t)min(i0 + i, p.parts - 1) * REC;
+            const float *r = rec + (size_t)min(i0 + i, used - 1) * REC;
             ml[i] = *reinterpret_cast<const float2 *>(r);
             v[i] = *reinterpret_cast<const floatx4 *>(r + REC_HEAD + d0);
         }
-        used = min(p.parts, p.used[row]);
         float m = M;
 #pragma unroll
         for (int i = 0; i < NR; ++i)

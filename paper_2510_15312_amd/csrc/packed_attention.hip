@@ -31,12 +31,14 @@ struct PackedAttn {
     const int32_t *table, *row_off, *kv_len;
     void *out;
     int32_t group, tiles, parts, part_pages;   // tiles: items tiles of all sequences, at most
+    int32_t tile_is_seq;                       // a tile is all items of a sequence
     Divisor by_group, by_heads, by_tiles, by_q_heads;
     float scale_log2e;
     float *records;                            // [row][head][part][REC_HEAD + head_dim], parts > 1
     int32_t *used;                             // [row]: parts with a record
 };
 constexpr int REC_HEAD = 4;                    // maximum, sum, -, -
+constexpr int TILE_WAVES = 4, FEW_WAVES = 8;
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -103,14 +105,15 @@ template <typename T> __device__ __forceinline__ bool any_not_finite(const Frag<
 // in bfloat16, half of one in float32 (the halves of a fragment's pieces in two units, so that a read of 16 bytes a lane
 // touches every bank once).  K rows are taken in the order that leaves a lane with eight consecutive keys per operand of
 // the second product: row m of a 32-key tile is key 16 (m >> 4) + 8 (m >> 2 & 1) + 4 (m >> 3 & 1) + (m & 3).
-template <typename T, int HD, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAttn p) {
-    constexpr int BM = WAVES * 32, HALVES = sizeof(T) / 2, UNITS = HD / 4 * HALVES, LPW = UNITS / WAVES;   // units of a page
+template <typename T, int HD, int KG>
+__global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kernel(PackedAttn p) {
+    constexpr int WAVES = TILE_WAVES, BM = WAVES * 32, HALVES = sizeof(T) / 2, UNITS = HD / 4 * HALVES, LPW = UNITS / WAVES;   // units of a page
     constexpr int KD = HD / 32, KS = HD / 16, DB = HD / 32;
     static_assert(UNITS % (2 * WAVES) == 0, "a wavefront loads K or V");
     extern __shared__ __align__(1024) unsigned char smem[];
     const vf_packed_args &a = p.a;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int wave = any_wave % WAVES, kg = any_wave / WAVES, tid = threadIdx.x % (WAVES * 64);   // within the group of wavefronts kg
     const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, part = p.by_tiles(rest), place = rest - part * p.tiles;
     const Tile t = find_tile<BM>(p, p.tiles - 1 - place);
     if (t.rows <= 0) return;
@@ -126,7 +129,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     const int wave_first = min(first_pos + p.by_group(min(n_items - 1, wave0)), cap - 1);
     const int pages = tile_last < 0 ? 0 : tile_last / VF_TILE + 1;
     const int p_begin = part * p.part_pages, p_end = part == p.parts - 1 ? pages : min(pages, p_begin + p.part_pages);
-    if (p.parts > 1 && part == 0 && kvh == 0 && wave0 + col < n_items && half == 0 && item_head == 0)
+    if (p.parts > 1 && part == 0 && kvh == 0 && wave0 + col < n_items && half == 0 && kg == 0 && item_head == 0)
         p.used[row] = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
     if (p_begin >= p_end && part > 0) return;
 
@@ -143,7 +146,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     const size_t page_bytes = (size_t)2 * a.n_kv_heads * VF_TILE * HD * sizeof(T);
     const char *src = (const char *)p.kv + (size_t)(wave < WAVES / 2 ? kvh : a.n_kv_heads + kvh) * (VF_TILE * HD * sizeof(T)) +
                       wave % (WAVES / 2) * (LPW * 1024);
-    const unsigned lds0 = lds_address(smem) + wave * (LPW * 1024);
+    unsigned char *const pages_lds = smem + kg * (2 * UNITS * 1024);
+    const unsigned lds0 = lds_address(pages_lds) + wave * (LPW * 1024);
     const int32_t *table = p.table + (size_t)t.seq * a.table_stride;
     // ids of 64 pages, one per lane: those from ids_at on
     int ids_at = p_begin, ids = table[min(p_begin + lane, a.max_pages - 1)];
@@ -155,12 +159,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
         const int id = __builtin_amdgcn_readlane(ids, pg - ids_at);
         return (unsigned)id < (unsigned)a.pool_pages ? id : -1;
     };
-    // K of page i + 1 and V of page i travel together, one step ahead of their use: a wavefront brings K or V
+    // Step i takes page p_begin + KG i + kg.  K of step i + 1 and V of step i travel together, one step ahead of their use: a
+    // wavefront brings K or V.
     auto issue = [&](int i) {
-        const int pg = p_begin + i + (wave < WAVES / 2 ? 1 : 0);
-        const int id = page_id(max(p_begin, min(pg, p_end - 1)));   // a page that is not needed: some page, not used
+        const int step = i + (wave < WAVES / 2 ? 1 : 0);
+        const int id = page_id(max(p_begin, min(p_begin + step * KG + kg, p_end - 1)));   // a page that is not needed: some page, not used
         const char *from = src + (size_t)max(id, 0) * page_bytes;
-        const unsigned dst = lds0 + (unsigned)(pg & 1) * (UNITS * 1024);
+        const unsigned dst = lds0 + (unsigned)(step & 1) * (UNITS * 1024);
         static_for<0, LPW>([&](auto f) {
             constexpr int F = f;
             if constexpr (HALVES == 1) fragment_to_lds<F * 1024>(from + F * 1024, lane * 16, dst);
@@ -288,7 +293,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
     };
     // Memory behind the last key may hold anything: its values count as zeros.
     auto clear_behind = [&](unsigned char *st, int keys) {   // keys: of the page that are there
-        for (int u = threadIdx.x; u < UNITS / 2 * 64; u += WAVES * 64) {
+        for (int u = tid; u < UNITS / 2 * 64; u += WAVES * 64) {
             const int piece = HALVES == 1 ? u : (u >> 7 << 6) + (u & 63), e0 = HALVES == 1 ? 0 : (u >> 6 & 1) * 4;
             const int there = keys - (piece / (DB * 128) * 32 + (piece >> 4 & 3) * 8) - e0;   // of this unit's 16 / sizeof(T) elements
             if (there >= 16 / (int)sizeof(T)) continue;
@@ -298,26 +303,26 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
                 if (j >= there) x[j] = from_f32<T>(0.f);
         }
     };
-    // Steps: page i's weights and products, and the scores of page i + 1, which do not wait for them.
-    const int n = p_end - p_begin;
+    // A step: a page's weights and products, and the scores of the next step's page, which do not wait for them.
+    const int n = (p_end - p_begin + KG - 1) / KG;
     if (n > 0) {
         // pages that all items see whole, up to the first that is not in the pool
-        int n_full = max(0, min(n, (tile_first + 1) / VF_TILE - p_begin));
-        for (int i0 = 0; i0 < n_full; i0 += 64) {
-            const int id = i0 ? table[p_begin + min(i0 + lane, n_full - 1)] : ids;
-            const unsigned long long missing = __builtin_amdgcn_ballot_w64(i0 + lane < n_full && (unsigned)id >= (unsigned)a.pool_pages);
-            if (missing) n_full = min(n_full, i0 + __builtin_ctzll(missing));
+        int full = max(0, min(p_end - p_begin, (tile_first + 1) / VF_TILE - p_begin));
+        for (int i0 = 0; i0 < full; i0 += 64) {
+            const int id = i0 ? table[p_begin + min(i0 + lane, full - 1)] : ids;
+            const unsigned long long missing = __builtin_amdgcn_ballot_w64(i0 + lane < full && (unsigned)id >= (unsigned)a.pool_pages);
+            if (missing) full = min(full, i0 + __builtin_ctzll(missing));
         }
-        auto k_page = [&](int i) { return smem + ((p_begin + i) & 1) * (UNITS * 1024); };
-        auto step = [&](int i) {   // behind it K of page i + 1 and V of page i have landed, and their slots' neighbours are free
+        const int n_full = full / KG;
+        auto k_page = [&](int i) { return pages_lds + (i & 1) * (UNITS * 1024); };
+        auto step = [&](int i) {   // behind it K of step i + 1 and V of step i have landed, and their slots' neighbours are free
             vm_wait<0>();
             lds_sync();
             issue(i + 1);
         };
         auto tail = [&](int i) {   // behind a step past n_full
-            const int keys = cap - (p_begin + i) * VF_TILE;
-            if (keys < VF_TILE) {
-                clear_behind(smem + ((p_begin + i) & 1) * (UNITS * 1024), keys);
+            if (cap - (p_begin + i * KG) * VF_TILE < VF_TILE * KG) {   // a page of the step is not full
+                clear_behind(k_page(i), cap - (p_begin + i * KG + kg) * VF_TILE);
                 lds_sync();
             }
         };
@@ -361,8 +366,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
                 }
             }
             for (; i < n; ++i) {
-                const int t0 = (p_begin + i) * VF_TILE;
-                const bool mine = t0 <= wave_last && page_id(p_begin + i) >= 0;
+                const int pg = p_begin + i * KG + kg, t0 = pg * VF_TILE;
+                const bool mine = pg < p_end && t0 <= wave_last && page_id(min(pg, p_end - 1)) >= 0;
                 Scores sc;
                 if (mine) sc = scores(k_page(i));
                 step(i);
@@ -377,6 +382,27 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_tiles_kernel(PackedAt
             }
         }
         vm_wait<0>();   // nothing is on its way to LDS when the workgroup ends
+    }
+    if constexpr (KG == 2) {   // the second group's sums join the first's
+        float *const at = reinterpret_cast<float *>(smem) + wave * (DB * 16 + 2) * 64 + lane;
+        lds_sync();
+        if (kg == 1) {
+            at[0] = m_run;
+            at[64] = l_run;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) at[(2 + db * 16 + i) * 64] = acc[db][i];
+        }
+        lds_sync();
+        if (kg == 1) return;
+        const float m = fmaxf(m_run, at[0]), own = __builtin_amdgcn_exp2f(m_run - m), other = __builtin_amdgcn_exp2f(at[0] - m);
+        m_run = m;
+        l_run = l_run * own + at[64] * other;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] = acc[db][i] * own + at[(2 + db * 16 + i) * 64] * other;
     }
     const float sum = l_run + __shfl_xor(l_run, 32, 64);
     if (wave0 + col >= n_items) return;
@@ -433,15 +459,26 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
     float *maxima = sums + WAVES * BM * OUT, *totals = maxima + WAVES * BM;
     const vf_packed_args &a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g4 = lane >> 4, l15 = lane & 15;
-    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, part = p.by_tiles(rest), seq = rest - part * p.tiles;
+    const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, part = p.by_tiles(rest), place = rest - part * p.tiles;
     const int p_first = part * p.part_pages;
-    const int32_t *table = p.table + (size_t)seq * a.table_stride;
-    int ids = table[min(p_first + lane, a.max_pages - 1)];   // asked for with the lengths
-    const int2 r = seq_rows(p, seq);
-    const int row0 = __builtin_amdgcn_readfirstlane(r.x), rows = __builtin_amdgcn_readfirstlane(r.y), kv_len = __builtin_amdgcn_readfirstlane(p.kv_len[seq]);
+    Tile t = {place, 0, 0, 0, 0};
+    int ids;   // of the part's first 64 pages, one per lane
+    if (p.tile_is_seq) {   // all items of a sequence, a tile after the other (mostly there is one)
+        ids = p.table[(size_t)place * a.table_stride + min(p_first + lane, a.max_pages - 1)];   // asked for with the lengths
+        const int2 r = seq_rows(p, place);
+        t.row0 = __builtin_amdgcn_readfirstlane(r.x);
+        t.rows = __builtin_amdgcn_readfirstlane(r.y);
+        t.kv_len = __builtin_amdgcn_readfirstlane(p.kv_len[place]);
+    } else {
+        t = find_tile<BM>(p, p.tiles - 1 - place);
+        ids = p.table[(size_t)t.seq * a.table_stride + min(p_first + lane, a.max_pages - 1)];
+    }
+    const int32_t *table = p.table + (size_t)t.seq * a.table_stride;
+    const int row0 = t.row0, rows = t.rows, kv_len = t.kv_len;
     const int group = p.group, n_items = rows * group, cap = min(kv_len, a.max_pages * VF_TILE), first_pos = kv_len - rows;
     const size_t page_bytes = (size_t)2 * a.n_kv_heads * VF_TILE * HD * sizeof(T), head_bytes = (size_t)VF_TILE * HD * sizeof(T);
-    for (int item0 = 0; item0 < n_items; item0 += BM) {
+    const int items_end = p.tile_is_seq ? n_items : min(n_items, t.item0 + BM);
+    for (int item0 = t.item0; item0 < items_end; item0 += BM) {
         const int last = min(first_pos + p.by_group(min(n_items - 1, item0 + BM - 1)), cap - 1);   // last key that an item sees
         const int pages = last < 0 ? 0 : last / VF_TILE + 1, parts = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
         const int p_end = part == p.parts - 1 ? pages : min(pages, p_first + p.part_pages);
@@ -471,7 +508,8 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
         // keys 32 i .. + 31, i = 2 p_first + wave, + WAVES ..
         const int first_all = min(first_pos + p.by_group(item0), cap - 1);   // last key that all items see
         const int i_end = min(2 * p_end, last / 32 + 1);
-        int ids_at = p_first;
+        int ids_at = p_first;   // (a second tile starts over)
+        if (item0 != t.item0) ids = table[min(p_first + lane, a.max_pages - 1)];
         Frag<T> k[2 * KD], v[DB];   // a tile's keys are asked for when those before have been multiplied, its values likewise
         auto page = [&](int i) {    // page id of tile i, -1: not in the pool
             const int pg = i / 2;
@@ -585,7 +623,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
             load_v(i_next, id_next);
         }
         // sums of the wavefronts; a lane's values: item l15, d = 16 db + 4 g4 + r
-        if (item0) __syncthreads();
+        if (item0 != t.item0) __syncthreads();
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             float l = l_run[nb];
@@ -699,26 +737,27 @@ int check(const char *name, const vf_packed_args *args) {
 }
 
 // Kernel, tiles and parts of a call, from what the host knows.
-struct Plan { int few, tiles, parts, part_pages; size_t bytes; };   // few: blocks of 16 items of attention_few_kernel, 0: attention_tiles_kernel
-
-constexpr int TILE_WAVES = 4, FEW_WAVES = 8;
+struct Plan { int few, tile_is_seq, key_groups, tiles, parts, part_pages; size_t bytes; };   // few: blocks of 16 items of attention_few_kernel, 0: attention_tiles_kernel
 
 Plan make_plan(const vf_packed_args &a) {
     Plan r{};
     const int group = a.n_q_heads / a.n_kv_heads;
     const int pages = std::max(1, std::min(a.max_pages, (int)(((long long)a.max_keys + VF_TILE - 1) / VF_TILE)));
     const long long most_items = (long long)std::min(a.max_rows, a.total_rows) * group, items = (long long)a.total_rows * group;
-    long long groups;
-    if (most_items <= (a.head_dim == 64 ? 32 : 16)) {
+    const int seqs = std::min(a.n_seqs, a.total_rows);
+    auto tiles = [&](int bm) { return (int)(items / bm + seqs); };   // a sequence ends in one tile that is not full
+    auto groups = [&](int bm) { return std::max<long long>(1, std::min<long long>(tiles(bm), (items + bm - 1) / bm)) * a.n_kv_heads; };
+    const int most_few = a.dtype == VF_BF16 || a.head_dim == 64 ? 2 : 1;
+    if (most_items <= 16 * most_few) {
         r.few = most_items <= 16 ? 1 : 2;
+        r.tile_is_seq = 1;
         r.tiles = a.n_seqs;
-        groups = (long long)std::min(a.n_seqs, a.total_rows) * a.n_kv_heads;
-        r.parts = (int)std::max(1ll, std::min<long long>((512 + groups - 1) / groups, pages / 8));
+        const long long g = (long long)seqs * a.n_kv_heads;
+        r.parts = pages <= 16 ? 1 : (int)std::max(1ll, std::min<long long>({(256 + g - 1) / g, 16, pages / 4}));
     } else {
         const int bm = TILE_WAVES * 32;
-        r.tiles = (int)(items / bm + std::min(a.n_seqs, a.total_rows));   // a sequence ends in one tile that is not full
-        groups = std::max<long long>(1, std::min<long long>(r.tiles, (items + bm - 1) / bm)) * a.n_kv_heads;
-        r.parts = (int)std::max(1ll, std::min<long long>((512 + groups - 1) / groups, pages / 4));
+        r.tiles = tiles(bm);
+        r.parts = (int)std::max(1ll, std::min<long long>((512 + groups(bm) - 1) / groups(bm), pages / 4));
     }
     r.part_pages = (pages + r.parts - 1) / r.parts;
     r.parts = (pages + r.part_pages - 1) / r.part_pages;
@@ -742,14 +781,14 @@ template <typename T, int HD, int NB> int launch_few(const PackedAttn &p, hipStr
     VF_HIP(set);
     return start(attention_few_kernel<T, HD, FEW_WAVES, NB>, (long long)p.tiles * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
 }
-template <typename T, int HD> int launch_tiles(const PackedAttn &p, hipStream_t st) {
-    constexpr int LDS = 2 * HD / 4 * 1024 * (int)sizeof(T) / 2;
-    static const hipError_t set = hipFuncSetAttribute((const void *)attention_tiles_kernel<T, HD, TILE_WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+template <typename T, int HD, int KG> int launch_tiles(const PackedAttn &p, hipStream_t st) {
+    constexpr int LDS = KG * 2 * HD / 4 * 1024 * (int)sizeof(T) / 2;
+    static const hipError_t set = hipFuncSetAttribute((const void *)attention_tiles_kernel<T, HD, KG>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     VF_HIP(set);
-    return start(attention_tiles_kernel<T, HD, TILE_WAVES>, (long long)p.tiles * p.parts * p.a.n_kv_heads, TILE_WAVES * 64, LDS, p, st);
+    return start(attention_tiles_kernel<T, HD, KG>, (long long)p.tiles * p.parts * p.a.n_kv_heads, TILE_WAVES * KG * 64, LDS, p, st);
 }
 template <typename T, int HD> int launch(const PackedAttn &p, const Plan &plan, hipStream_t st) {
-    const int rc = plan.few == 1 ? launch_few<T, HD, 1>(p, st) : plan.few == 2 ? launch_few<T, HD, HD == 64 ? 2 : 1>(p, st) : launch_tiles<T, HD>(p, st);
+    const int rc = plan.few == 1 ? launch_few<T, HD, 1>(p, st) : plan.few == 2 ? launch_few<T, HD, sizeof(T) * HD <= 256 ? 2 : 1>(p, st) : plan.key_groups == 2 ? launch_tiles<T, HD, sizeof(T) * HD <= 256 ? 2 : 1>(p, st) : launch_tiles<T, HD, 1>(p, st);
     if (rc != VF_OK || p.parts == 1) return rc;
     constexpr int PER = 256 / (HD / 4);
     return start(attention_merge_kernel<T, HD>, ((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER, 256, 0, p, st);
@@ -786,6 +825,7 @@ int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const voi
     p.out = out_dev;
     p.group = p.a.n_q_heads / p.a.n_kv_heads;
     p.tiles = plan.tiles;
+    p.tile_is_seq = plan.tile_is_seq;
     p.parts = plan.parts;
     p.part_pages = plan.part_pages;
     p.scale_log2e = (p.a.scale == 0.f ? 1.0f / sqrtf((float)p.a.head_dim) : p.a.scale) * 1.4426950408889634f;

@@ -99,6 +99,14 @@ template <typename T> __device__ __forceinline__ bool any_not_finite(const Frag<
     return bad;
 }
 
+// Four kilobytes apart by OFF from memory straight to LDS, free to be moved by the compiler: a statement takes `order` and hands it on.
+// The destination goes through m0 (one idle cycle before the load); an instruction's own offset counts for both addresses.
+template <int OFF> __device__ __forceinline__ int unit_to_lds(int order, const void *src, unsigned lane_off, unsigned lds) {
+    if constexpr (OFF == 0) asm("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : "+s"(order) : "s"(lds), "v"(lane_off), "s"(src));
+    else asm("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 offset:%4" : "+s"(order) : "s"(lds), "v"(lane_off), "s"(src), "n"(OFF));
+    return order;
+}
+
 // Tiles of 32 items a wavefront, pages of 64 keys through LDS.
 //
 // A page comes as direct loads of 1 KB units.  Units hold 16 bytes a lane: a K or V piece of eight elements
@@ -161,16 +169,29 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
     };
     // Step i takes page p_begin + KG i + kg.  K of step i + 1 and V of step i travel together, one step ahead of their use: a
     // wavefront brings K or V.
-    auto issue = [&](int i) {
+    // The loads' statements are tied to the step's barrier by `order`, which each takes and hands on, and are otherwise free to
+    // stand among the products (a volatile statement is a fence for every LDS read: 200 cycles in front of the first product).
+    int order = 0;
+    struct Source { const char *from; unsigned dst; };
+    auto source = [&](int i) {
         const int step = i + (wave < WAVES / 2 ? 1 : 0);
         const int id = page_id(max(p_begin, min(p_begin + step * KG + kg, p_end - 1)));   // a page that is not needed: some page, not used
-        const char *from = src + (size_t)max(id, 0) * page_bytes;
-        const unsigned dst = lds0 + (unsigned)(step & 1) * (UNITS * 1024);
-        static_for<0, LPW>([&](auto f) {
-            constexpr int F = f;
-            if constexpr (HALVES == 1) fragment_to_lds<F * 1024>(from + F * 1024, lane * 16, dst);
-            else fragment_to_lds<F * 1024>(from + F / 2 * 2048 + F % 2 * 16, lane * 32, dst);
-        });
+        return Source{src + (size_t)max(id, 0) * page_bytes, lds0 + (unsigned)(step & 1) * (UNITS * 1024)};
+    };
+    auto issue_unit = [&](const Source &x, auto f) {
+        constexpr int F = f;
+        const unsigned off = HALVES == 1 ? lane * 16 : lane * 32;
+        if constexpr (HALVES == 1) order = unit_to_lds<F % 4 * 1024>(order, x.from + F / 4 * 4096, off, x.dst + F / 4 * 4096);
+        else order = unit_to_lds<0>(order, x.from + F / 2 * 2048 + F % 2 * 16, off, x.dst + F * 1024);
+    };
+    auto issue = [&](int i) {
+        const Source x = source(i);
+        static_for<0, LPW>([&](auto f) { issue_unit(x, f); });
+    };
+    auto landed = [&](auto left) {   // until at most `left` of this wavefront's loads are outstanding, then the workgroup's barrier
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"((int)left), "s"(order) : "memory");
+        lds_sync();
+        asm volatile("" : "+s"(order) : : "memory");
     };
     // a lane's pieces: K row col of a 32-key tile, V^T row col of 32 output dimensions
     const unsigned k_lane = (unsigned)((col >> 3 & 1) * KD * 64 * HALVES + half * 16 + (col >> 4) * 8 + (col >> 2 & 1) * 4 + (col & 3)) * 16;
@@ -316,8 +337,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
         const int n_full = full / KG;
         auto k_page = [&](int i) { return pages_lds + (i & 1) * (UNITS * 1024); };
         auto step = [&](int i) {   // behind it K of step i + 1 and V of step i have landed, and their slots' neighbours are free
-            vm_wait<0>();
-            lds_sync();
+            landed(std::integral_constant<int, 0>{});
             issue(i + 1);
         };
         auto tail = [&](int i) {   // behind a step past n_full
@@ -328,8 +348,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
         };
         issue(-1);
         issue(0);
-        vm_wait<LPW>();
-        lds_sync();
+        landed(std::integral_constant<int, LPW>{});
         if (!has_items) {
             for (int i = 0; i < n; ++i) {
                 step(i);
@@ -381,7 +400,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
                 products_masked(k_page(i), t0);
             }
         }
-        vm_wait<0>();   // nothing is on its way to LDS when the workgroup ends
+        asm volatile("s_waitcnt vmcnt(0)" : : "s"(order) : "memory");   // nothing is on its way to LDS when the workgroup ends
     }
     if constexpr (KG == 2) {   // the second group's sums join the first's
         float *const at = reinterpret_cast<float *>(smem) + wave * (DB * 16 + 2) * 64 + lane;

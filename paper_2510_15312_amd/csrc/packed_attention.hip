@@ -38,7 +38,7 @@ struct PackedAttn {
     int32_t *used;                             // [row]: parts with a record
 };
 constexpr int REC_HEAD = 4;                    // maximum, sum, -, -
-constexpr int TILE_WAVES = 4, FEW_WAVES = 8;
+constexpr int TILE_WAVES = 4, FEW_WAVES = 8, FEW_ITEMS = 16;
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
         }
 }
 
-// Few items of a sequence (single tokens, short drafts): a workgroup takes 16 NB items at a time of one sequence and key head over
+// Few items (single tokens, drafts, short prompts): a workgroup takes 16 items of one sequence and key head over
 // one part of the keys, its wavefronts the part's tiles of 32 keys in turn, straight from memory into registers: every K and V
 // fragment of the pool is one contiguous kilobyte.  The wavefronts' sums meet in LDS.
 // Operands of a 16x16 product over 32 values of k: 16 lanes each take 8.
@@ -471,9 +471,9 @@ template <typename T> __device__ __forceinline__ Frag<T> load_frag(const char *a
     return f;
 }
 
-template <typename T, int HD, int WAVES, int NB>
-__global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kernel(PackedAttn p) {
-    constexpr int KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = 16 * NB, OUT = HD + 4;   // FRAG: bytes; OUT: stride of a sum in LDS
+template <typename T, int HD>
+__global__ __launch_bounds__(FEW_WAVES * 64) VF_MFMA_KERNEL void attention_few_kernel(PackedAttn p) {
+    constexpr int WAVES = FEW_WAVES, KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = FEW_ITEMS, OUT = HD + 4;   // FRAG: bytes; OUT: stride of a sum in LDS
     extern __shared__ __align__(16) float sums[];   // [WAVES][BM][OUT], then maxima and sums of weights
     float *maxima = sums + WAVES * BM * OUT, *totals = maxima + WAVES * BM;
     const vf_packed_args &a = p.a;
@@ -504,26 +504,15 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
         if (p.parts > 1 && part == 0 && kvh == 0 && threadIdx.x < BM && item0 + (int)threadIdx.x < n_items)
             p.used[row0 + p.by_group(item0 + threadIdx.x)] = parts;
         if (p_first >= p_end && part > 0) continue;
-        int last_key[NB];
-        Frag<T> qf[NB][KD];
+        Frag<T> qf[KD];
+        const int item = min(n_items - 1, item0 + l15), item_row = p.by_group(item), last_key = min(first_pos + item_row, cap - 1);
+        const T *q = (const T *)p.q + (row0 + item_row) * a.q_stride + (kvh * group + item - item_row * group) * HD + g4 * 8;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int item = min(n_items - 1, item0 + nb * 16 + l15);
-            const int item_row = p.by_group(item);
-            last_key[nb] = min(first_pos + item_row, cap - 1);
-            const T *q = (const T *)p.q + (row0 + item_row) * a.q_stride + (kvh * group + item - item_row * group) * HD + g4 * 8;
+        for (int kd = 0; kd < KD; ++kd) qf[kd] = load_frag<T>((const char *)(q + kd * 32));
+        floatx4 acc[DB];
+        float m_run = -1e30f, l_run = 0.f;
 #pragma unroll
-            for (int kd = 0; kd < KD; ++kd) qf[nb][kd] = load_frag<T>((const char *)(q + kd * 32));
-        }
-        floatx4 acc[NB][DB];
-        float m_run[NB], l_run[NB];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            m_run[nb] = -1e30f;
-            l_run[nb] = 0.f;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) acc[nb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
-        }
+        for (int db = 0; db < DB; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
         // keys 32 i .. + 31, i = 2 p_first + wave, + WAVES ..
         const int first_all = min(first_pos + p.by_group(item0), cap - 1);   // last key that all items see
         const int i_end = min(2 * p_end, last / 32 + 1);
@@ -561,29 +550,26 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
             id_next = page(i_next);
             const int own = i * 32 + g4 * 8;                // key of score j: own + j
             const bool masked = i * 32 + 31 > first_all;
-            float s[NB][8];
+            float s[8];
+            floatx4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                floatx4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            for (int kd = 0; kd < KD; ++kd)
 #pragma unroll
-                for (int kd = 0; kd < KD; ++kd)
+                for (int h = 0; h < 2; ++h) c[h] = mma16(k[h * KD + kd], qf[kd], c[h]);
+            float mx = -INFINITY;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) c[h] = mma16(k[h * KD + kd], qf[nb][kd], c[h]);
-                float mx = -INFINITY;
+            for (int j = 0; j < 8; ++j) {
+                s[j] = id < 0 || (masked && own + j > last_key) ? -INFINITY : c[j >> 2][j & 3];
+                mx = fmaxf(mx, s[j]);
+            }
+            mx *= p.scale_log2e;
+            if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f)) {   // with slack: see attention_tiles_kernel
+                mx = over_item(mx, [](float u, float v) { return fmaxf(u, v); });
+                const float m_new = fmaxf(m_run, mx), keep = __builtin_amdgcn_exp2f(m_run - m_new);
+                l_run *= keep;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    s[nb][j] = id < 0 || (masked && own + j > last_key[nb]) ? -INFINITY : c[j >> 2][j & 3];
-                    mx = fmaxf(mx, s[nb][j]);
-                }
-                mx *= p.scale_log2e;
-                if (__builtin_amdgcn_ballot_w64(mx > m_run[nb] + 8.f)) {   // with slack: see attention_tiles_kernel
-                    mx = over_item(mx, [](float u, float v) { return fmaxf(u, v); });
-                    const float m_new = fmaxf(m_run[nb], mx), keep = __builtin_amdgcn_exp2f(m_run[nb] - m_new);
-                    l_run[nb] *= keep;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) acc[nb][db] *= keep;
-                    m_run[nb] = m_new;
-                }
+                for (int db = 0; db < DB; ++db) acc[db] *= keep;
+                m_run = m_new;
             }
             load_k(i_next, id_next);
             // values of keys that nobody sees count as zeros; one that only some items see and that is not finite would reach
@@ -598,60 +584,54 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
                         bad |= own + j > first_all && not_finite(to_f32(v[db].v[j]));
                     }
             }
+            // bfloat16 weights as a sum of two (16 significant bits): the loads, not the products, are what this kernel waits for.
+            // The first is rounded towards zero and the second never zero beside it, so that an infinite value stays one.
+            Frag<T> hi, lo;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                // bfloat16 weights as a sum of two (16 significant bits): the loads, not the products, are what this kernel waits for.
-                // The first is rounded towards zero and the second never zero beside it, so that an infinite value stays one.
-                Frag<T> hi, lo;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float w = __builtin_amdgcn_exp2f(fmaf(s[nb][j], p.scale_log2e, -m_run[nb]));
-                    l_run[nb] += w;
-                    if constexpr (sizeof(T) == 2) {
-                        const float top = __uint_as_float(__float_as_uint(w) & 0xffff0000u);
-                        hi.v[j] = from_f32<T>(top);
-                        lo.v[j] = from_f32<T>(fmaxf(w - top, w * 0x1p-24f));
-                    } else {
-                        hi.v[j] = w;
-                    }
-                }
-                auto product = [&](const Frag<T> &x, floatx4 c) {
-                    c = mma16(x, hi, c);
-                    if constexpr (sizeof(T) == 2) c = mma16(x, lo, c);
-                    return c;
-                };
-                if (!__builtin_amdgcn_ballot_w64(bad)) {
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) acc[nb][db] = product(v[db], acc[nb][db]);
+            for (int j = 0; j < 8; ++j) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[j], p.scale_log2e, -m_run));
+                l_run += w;
+                if constexpr (sizeof(T) == 2) {
+                    const float top = __uint_as_float(__float_as_uint(w) & 0xffff0000u);
+                    hi.v[j] = from_f32<T>(top);
+                    lo.v[j] = from_f32<T>(fmaxf(w - top, w * 0x1p-24f));
                 } else {
-                    static_for<0, DB>([&](auto db) {
-                        floatx4 sum = acc[nb][(int)db];
-                        for (int seen = max(first_all, i * 32); seen <= min(last, i * 32 + 31); ++seen) {
-                            Frag<T> x = v[(int)db];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (own + j > seen) x.v[j] = from_f32<T>(0.f);
-                            const floatx4 c = product(x, acc[nb][(int)db]);
-                            if (min(last_key[nb], i * 32 + 31) == seen) sum = c;
-                        }
-                        acc[nb][(int)db] = sum;
-                        __builtin_amdgcn_sched_barrier(0);
-                    });
+                    hi.v[j] = w;
                 }
+            }
+            auto product = [&](const Frag<T> &x, floatx4 sum) {
+                sum = mma16(x, hi, sum);
+                if constexpr (sizeof(T) == 2) sum = mma16(x, lo, sum);
+                return sum;
+            };
+            if (!__builtin_amdgcn_ballot_w64(bad)) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = product(v[db], acc[db]);
+            } else {
+                static_for<0, DB>([&](auto db) {
+                    constexpr int D = db;
+                    floatx4 sum = acc[D];
+                    for (int seen = max(first_all, i * 32); seen <= min(last, i * 32 + 31); ++seen) {
+                        Frag<T> x = v[D];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (own + j > seen) x.v[j] = from_f32<T>(0.f);
+                        const floatx4 of_row = product(x, acc[D]);
+                        if (min(last_key, i * 32 + 31) == seen) sum = of_row;
+                    }
+                    acc[D] = sum;
+                    __builtin_amdgcn_sched_barrier(0);   // one block's values in registers at a time
+                });
             }
             load_v(i_next, id_next);
         }
         // sums of the wavefronts; a lane's values: item l15, d = 16 db + 4 g4 + r
         if (item0 != t.item0) __syncthreads();
+        const float l = over_item(l_run, [](float u, float v) { return u + v; });
+        const int at = wave * BM + l15;
+        if (g4 == 0) { maxima[at] = m_run; totals[at] = l; }
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            float l = l_run[nb];
-            l = over_item(l, [](float u, float v) { return u + v; });
-            const int at = wave * BM + nb * 16 + l15;
-            if (g4 == 0) { maxima[at] = m_run[nb]; totals[at] = l; }
-#pragma unroll
-            for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4 *>(&sums[at * OUT + db * 16 + g4 * 4]) = acc[nb][db];
-        }
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4 *>(&sums[at * OUT + db * 16 + g4 * 4]) = acc[db];
         __syncthreads();
         for (int j = threadIdx.x; j < BM * (HD / 4); j += WAVES * 64) {
             const int it = j / (HD / 4), d0 = j % (HD / 4) * 4, item = item0 + it;
@@ -755,34 +735,62 @@ int check(const char *name, const vf_packed_args *args) {
     return VF_OK;
 }
 
-// Kernel, tiles and parts of a call, from what the host knows.
-struct Plan { int few, tile_is_seq, key_groups, tiles, parts, part_pages; size_t bytes; };   // few: blocks of 16 items of attention_few_kernel, 0: attention_tiles_kernel
+// ---- choice of kernel and parts -------------------------------------------------------------------
+
+enum { TILES = 0, TILES_TWO = 1, FEW = 2, N_KERNELS = 3 };   // 128 items a workgroup; the same, two groups of wavefronts; 16 items
+struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages; size_t bytes; };
+
+// What a call costs, in us: the way of the longest workgroup through its pages, what is more than the chip holds, and a merge.
+// The constants are fits to 176 calls (prompts, chunks behind a prefix, drafts and single tokens of 1 to 64 sequences in four
+// shapes, with every kernel and the numbers of parts below: profiles/packed_attention_plan_timings.txt); the choice costs 1.4 %
+// on average against the best of all (tiles of 128 items without parts throughout: 229 %), 14 % at most.
+struct KernelCost {
+    float start, page, page_full;   // page: with up to half as many workgroups as the chip holds; page_full: with as many and more
+    float more, more_start;         // for every further chip full: a page, a workgroup
+};
+struct TypeCost { KernelCost k[N_KERNELS]; float merge, merge_mb, merge8; };
+constexpr TypeCost COST[3] = {
+    {{{1.759f, 1.543f, 1.223f, 0.8654f, 1.002f}, {6.108f, 0.5364f, 0.6751f, 0.4049f, 2.977f}, {3.053f, 0.2486f, 0.4449f, 0.1005f, 2.478f}}, 3.832f, 0.4793f, 1.042f},   // bfloat16, heads of 64
+    {{{5.5f, 0.9f, 1.273f, 1.247f, 3.701f}, {6.783f, 0.8328f, 0.6975f, 0.6541f, 5.996f}, {4.43f, 0.3524f, 0.6176f, 0.199f, 3.766f}}, 4.463f, 0.4145f, 1.76f},   // bfloat16, heads of 128
+    {{{5.592f, 4.087f, 9.576f, 0.8124f, 2.904f}, {}, {5.655f, 0.6763f, 0.9135f, 1.002f, 1.447f}}, 2.728f, 0.9495f, 1.344f},   // float32
+};
 
 Plan make_plan(const vf_packed_args &a) {
-    Plan r{};
-    const int group = a.n_q_heads / a.n_kv_heads;
+    Plan best{};
+    const TypeCost &cost = COST[a.dtype == VF_F32 ? 2 : a.head_dim == 64 ? 0 : 1];
+    const int group = a.n_q_heads / a.n_kv_heads, seqs = std::min(a.n_seqs, a.total_rows);
     const int pages = std::max(1, std::min(a.max_pages, (int)(((long long)a.max_keys + VF_TILE - 1) / VF_TILE)));
     const long long most_items = (long long)std::min(a.max_rows, a.total_rows) * group, items = (long long)a.total_rows * group;
-    const int seqs = std::min(a.n_seqs, a.total_rows);
-    auto tiles = [&](int bm) { return (int)(items / bm + seqs); };   // a sequence ends in one tile that is not full
-    auto groups = [&](int bm) { return std::max<long long>(1, std::min<long long>(tiles(bm), (items + bm - 1) / bm)) * a.n_kv_heads; };
-    const int most_few = a.dtype == VF_BF16 || a.head_dim == 64 ? 2 : 1;
-    if (most_items <= 16 * most_few) {
-        r.few = most_items <= 16 ? 1 : 2;
-        r.tile_is_seq = 1;
-        r.tiles = a.n_seqs;
-        const long long g = (long long)seqs * a.n_kv_heads;
-        r.parts = pages <= 16 ? 1 : (int)std::max(1ll, std::min<long long>({(256 + g - 1) / g, 16, pages / 4}));
-    } else {
-        const int bm = TILE_WAVES * 32;
-        r.tiles = tiles(bm);
-        r.parts = (int)std::max(1ll, std::min<long long>((512 + groups(bm) - 1) / groups(bm), pages / 4));
+    // pages that an item sees on average: rows do not see the call's later ones (how much shorter the other sequences are than
+    // the longest the host does not say)
+    const float whole = std::min(1.f, (float)a.max_rows / std::max(1, a.max_keys));
+    const float mean = std::max(1.f, pages * (1.f - 0.5f * whole));
+    float best_cost = 0.f;
+    for (int kernel = 0; kernel < N_KERNELS; ++kernel) {
+        if (kernel == TILES_TWO && a.dtype == VF_F32) continue;   // one wavefront's float32 products fill a matrix unit
+        if (kernel != FEW && most_items <= FEW_ITEMS) continue;     // every sequence one tile of 16: bound by memory, and more exact there
+        const int bm = kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32, chip = kernel == TILES ? 512 : 256;   // workgroups on 256 CUs
+        const KernelCost &k = cost.k[kernel];
+        const bool tile_is_seq = kernel == FEW && most_items <= bm;
+        const float groups = (tile_is_seq ? seqs : items / (float)bm + (seqs > 1 ? 0.5f * seqs : 0.5f)) * a.n_kv_heads;
+        for (const int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+            const int part_pages = (pages + parts - 1) / parts;
+            if ((pages + part_pages - 1) / part_pages != parts) continue;
+            const float used = parts == 1 ? 1.f : std::min((float)parts, mean / part_pages + 1.f);
+            const float workgroups = groups * used, half = 0.5f * chip;
+            float us = k.start + part_pages * (k.page + (k.page_full - k.page) * std::min(1.f, std::max(0.f, workgroups / half - 1.f))) +
+                       std::max(0.f, workgroups / chip - 1.f) * (k.more * mean / used + k.more_start);
+            if (parts > 1) us += cost.merge + cost.merge_mb * 4e-6f * a.total_rows * a.n_q_heads * used * (REC_HEAD + a.head_dim) + cost.merge8 * (((int)used - 1) / 8);
+            if (best.parts && us >= best_cost) continue;
+            best_cost = us;
+            best = {kernel, tile_is_seq, 0, parts, part_pages, 0};
+        }
     }
-    r.part_pages = (pages + r.parts - 1) / r.parts;
-    r.parts = (pages + r.part_pages - 1) / r.part_pages;
-    if (r.parts > 1)
-        r.bytes = (size_t)a.total_rows * a.n_q_heads * r.parts * (REC_HEAD + a.head_dim) * sizeof(float) + (size_t)a.total_rows * sizeof(int32_t);
-    return r;
+    const int bm = best.kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32;
+    best.tiles = best.tile_is_seq ? a.n_seqs : (int)(items / bm + seqs);   // a sequence ends in one tile that is not full
+    if (best.parts > 1)
+        best.bytes = (size_t)a.total_rows * a.n_q_heads * best.parts * (REC_HEAD + a.head_dim) * sizeof(float) + (size_t)a.total_rows * sizeof(int32_t);
+    return best;
 }
 
 // Workgroups in the order of their numbers: the first parts of all tiles (those that exist for all), then the second .. A die takes every
@@ -794,11 +802,11 @@ template <typename F> int start(F kernel, long long blocks, int threads, int lds
     VF_LAUNCH_CHECK("attention_packed");
     return VF_OK;
 }
-template <typename T, int HD, int NB> int launch_few(const PackedAttn &p, hipStream_t st) {
-    constexpr int LDS = FEW_WAVES * 16 * NB * (HD + 6) * 4;
-    static const hipError_t set = hipFuncSetAttribute((const void *)attention_few_kernel<T, HD, FEW_WAVES, NB>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+template <typename T, int HD> int launch_few(const PackedAttn &p, hipStream_t st) {
+    constexpr int LDS = FEW_WAVES * FEW_ITEMS * (HD + 6) * 4;
+    static const hipError_t set = hipFuncSetAttribute((const void *)attention_few_kernel<T, HD>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     VF_HIP(set);
-    return start(attention_few_kernel<T, HD, FEW_WAVES, NB>, (long long)p.tiles * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
+    return start(attention_few_kernel<T, HD>, (long long)p.tiles * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
 }
 template <typename T, int HD, int KG> int launch_tiles(const PackedAttn &p, hipStream_t st) {
     constexpr int LDS = KG * 2 * HD / 4 * 1024 * (int)sizeof(T) / 2;
@@ -807,7 +815,7 @@ template <typename T, int HD, int KG> int launch_tiles(const PackedAttn &p, hipS
     return start(attention_tiles_kernel<T, HD, KG>, (long long)p.tiles * p.parts * p.a.n_kv_heads, TILE_WAVES * KG * 64, LDS, p, st);
 }
 template <typename T, int HD> int launch(const PackedAttn &p, const Plan &plan, hipStream_t st) {
-    const int rc = plan.few == 1 ? launch_few<T, HD, 1>(p, st) : plan.few == 2 ? launch_few<T, HD, sizeof(T) * HD <= 256 ? 2 : 1>(p, st) : plan.key_groups == 2 ? launch_tiles<T, HD, sizeof(T) * HD <= 256 ? 2 : 1>(p, st) : launch_tiles<T, HD, 1>(p, st);
+    const int rc = plan.kernel == FEW ? launch_few<T, HD>(p, st) : plan.kernel == TILES ? launch_tiles<T, HD, 1>(p, st) : launch_tiles<T, HD, sizeof(T) == 2 ? 2 : 1>(p, st);
     if (rc != VF_OK || p.parts == 1) return rc;
     constexpr int PER = 256 / (HD / 4);
     return start(attention_merge_kernel<T, HD>, ((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER, 256, 0, p, st);
@@ -816,6 +824,15 @@ template <typename T, int HD> int launch(const PackedAttn &p, const Plan &plan, 
 }  // namespace
 
 extern "C" {
+
+// Which kernel and how many parts a call takes: for the test that holds the choice against kept timings.
+int vf_debug_packed_plan(const vf_packed_args *args, int *kernel, int *parts) {
+    if (const int rc = check("vf_debug_packed_plan", args)) return rc;
+    const Plan plan = make_plan(*args);
+    *kernel = plan.kernel;
+    *parts = plan.parts;
+    return VF_OK;
+}
 
 size_t vf_attention_packed_workspace(const vf_packed_args *args) {
     if (check("vf_attention_packed_workspace", args) != VF_OK) return (size_t)-1;

@@ -1,0 +1,78 @@
+"""A batch of requests served from one page pool: the host's side of the packed operators.
+
+A step gives every request some more tokens (a whole prompt, a chunk of one, drafts, one token, none), packed row behind row.
+`begin` takes their pages from the free list (`vf_pages_assign`), `attend` stores a layer's keys and values and attends over the
+cache (`vf_rotary_append`, `vf_attention_packed`), `finish` tells which requests had room: one copy of a few integers, the
+step's one synchronisation.  `keep` takes back tokens that were not accepted, `release` gives a request's pages back.
+The projections around `attend`, the norms and the feed-forward are the caller's.
+"""
+import torch
+
+from . import binding as vf
+
+PAGE = 64
+
+
+class PackedBatch:
+    def __init__(self, n_requests, n_layers, n_q_heads, n_kv_heads, head_dim, pool_pages, max_tokens, dtype=torch.bfloat16,
+                 rotary_dim=None, theta=1e6, pairs=vf.VF_ROTARY_HALF, device="cuda:0"):
+        """Room for n_requests requests of at most max_tokens tokens each, in pool_pages pages of 64 tokens together."""
+        def ints(*shape, value=0):
+            return torch.full(shape, value, dtype=torch.int32, device=device)
+        self.heads, self.pairs, self.device = (n_q_heads, n_kv_heads, head_dim), pairs, device
+        self.max_pages = -(-max_tokens // PAGE)
+        self.pools = torch.zeros((n_layers, pool_pages, 2, n_kv_heads, PAGE * head_dim), dtype=dtype, device=device)
+        self.angles = vf.vf_rotary_table(rotary_dim or head_dim, theta, PAGE * self.max_pages, device=device)
+        self.table = ints(n_requests, self.max_pages, value=-1)
+        self.free = torch.arange(pool_pages, dtype=torch.int32, device=device)
+        self.n_free, self.n_free_after = ints(1, value=pool_pages), ints(1)
+        self.lens, self.row_off, self.kv_len = ints(n_requests), ints(n_requests + 1), ints(n_requests)
+        self.host_lens, self.host_free = [0] * n_requests, pool_pages
+
+    def begin(self, new):
+        """new[b] tokens for request b.  Returns the device's row offsets [n + 1] and the rows' positions (-1: refused)."""
+        self.new, rows = [int(w) for w in new], sum(max(0, int(w)) for w in new)
+        self.pos = torch.empty(rows, dtype=torch.int32, device=self.device)
+        self.slot = torch.empty_like(self.pos)
+        vf.vf_pages_assign(self.lens, torch.tensor(self.new, dtype=torch.int32, device=self.device), self.free, self.n_free,
+                           self.table, self.row_off, self.pos, self.slot, self.kv_len, self.n_free_after)
+        self.workspace, self.max_rows = None, max([0] + self.new)
+        self.max_keys = max(h + max(0, w) for h, w in zip(self.host_lens, self.new))
+        return self.row_off, self.pos
+
+    def attend(self, layer, q, k, v):
+        """q [rows, q heads, head_dim], k, v [rows, kv heads, head_dim] before rotation (views of one wider matrix allowed): stores
+        k and v, returns the attention of every row, zeros for the rows of a refused request."""
+        pool, rotated, out = self.pools[layer], q.new_empty(q.shape), q.new_empty(q.shape)
+        vf.vf_rotary_append(q, k, v, self.angles, self.pos, self.slot, rotated, pool, self.pairs)
+        if self.workspace is None:      # the layers of a step share it
+            self.workspace = vf.vf_attention_packed_workspace(rotated, pool, self.table, self.max_rows, self.max_keys)
+        vf.vf_attention_packed(rotated, pool, self.table, self.row_off, self.kv_len, out, self.max_rows, self.max_keys, self.workspace)
+        return out
+
+    def finish(self):
+        """Ends the step: the lengths move on, the free list is what is left.  Returns a truth value per request: False where
+        the pool or the table had no room, so that the request stands as before and may ask again."""
+        self.lens = torch.where(self.kv_len > 0, self.kv_len, self.lens)
+        self.n_free, self.n_free_after = self.n_free_after, self.n_free
+        *lens, self.host_free = torch.cat([self.kv_len, self.n_free]).tolist()
+        granted = [length > 0 or w == 0 for length, w in zip(lens, self.new)]
+        self.host_lens = [length or before for length, before in zip(lens, self.host_lens)]
+        return granted
+
+    def keep(self, request, tokens):
+        """Of the request's tokens the first `tokens` stay (drafts that were not accepted go); pages behind them are free again."""
+        first, last = -(-tokens // PAGE), -(-self.host_lens[request] // PAGE)
+        if not 0 <= tokens <= self.host_lens[request]:
+            raise ValueError(f"request {request} holds {self.host_lens[request]} tokens, not {tokens}")
+        if first < last:
+            self.free[self.host_free:self.host_free + last - first] = self.table[request, first:last]
+            self.table[request, first:last] = -1
+            self.host_free += last - first
+            self.n_free.fill_(self.host_free)
+        self.lens[request] = tokens
+        self.host_lens[request] = tokens
+
+    def release(self, request):
+        """The request is over: its place in the batch and its pages are free."""
+        self.keep(request, 0)

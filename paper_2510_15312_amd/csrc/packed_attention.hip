@@ -32,6 +32,7 @@ struct PackedAttn {
     void *out;
     int32_t group, tiles, parts, part_pages;   // tiles: items tiles of all sequences, at most
     int32_t tile_is_seq;                       // a tile is all items of a sequence
+    int32_t by_height;                         // tiles with the most keys first
     Divisor by_group, by_heads, by_tiles, by_q_heads;
     float scale_log2e;
     float *records;                            // [row][head][part][REC_HEAD + head_dim], parts > 1
@@ -48,27 +49,54 @@ __device__ __forceinline__ int2 seq_rows(const PackedAttn &p, int b) {   // firs
     const int r0 = min(max(p.row_off[b], 0), p.a.total_rows), r1 = min(max(p.row_off[b + 1], r0), p.a.total_rows);
     return {r0, r1 - r0};
 }
-// Tiles are counted sequence by sequence, 64 sequences at a time.
-template <int BM> __device__ __forceinline__ Tile find_tile(const PackedAttn &p, int tile) {
+// Over the wavefront's lanes, for values that are not negative: up to and with this lane.
+template <int CTRL, int ROWS, typename F> __device__ __forceinline__ int lane_step(int x, F f) {
+    return f(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false));
+}
+template <typename F> __device__ __forceinline__ int lanes_upto(int x, F f) {
+    x = lane_step<0x111, 0xf>(x, f);   // a row of 16 lanes: by 1, 2, 4, 8
+    x = lane_step<0x112, 0xf>(x, f);
+    x = lane_step<0x114, 0xf>(x, f);
+    x = lane_step<0x118, 0xf>(x, f);
+    x = lane_step<0x142, 0xa>(x, f);   // a row's last lane to the next row
+    return lane_step<0x143, 0xc>(x, f);   // lane 31 to the upper half
+}
+struct Plus { __device__ __forceinline__ int operator()(int x, int y) const { return x + y; } };
+struct Max { __device__ __forceinline__ int operator()(int x, int y) const { return max(x, y); } };
+// Tile number `tile` of all, 64 sequences at a time: sequence by sequence, or those with the most keys first (by_height).  A tile's
+// height is its place in its sequence, counted in tiles, cached tokens among them; as high as h or higher are clamp(end - h, 0, tiles)
+// of a sequence.
+template <int BM> __device__ __forceinline__ Tile find_tile(const PackedAttn &p, int tile, bool by_height) {
     const int lane = threadIdx.x & 63;
-    for (int b0 = 0, base = 0; b0 < p.a.n_seqs; b0 += 64) {
+    for (int b0 = 0; b0 < p.a.n_seqs; b0 += 64) {
         const int b = min(b0 + lane, p.a.n_seqs - 1);
         const int2 r = seq_rows(p, b);
         const int len = p.kv_len[b];
-        int upto = b0 + lane < p.a.n_seqs ? (int)(((long long)r.y * p.group + BM - 1) / BM) : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += x;
+        const int tiles = b0 + lane < p.a.n_seqs ? (int)(((long long)r.y * p.group + BM - 1) / BM) : 0;
+        const int upto = lanes_upto(tiles, Plus{}), all = __builtin_amdgcn_readlane(upto, 63);
+        if (tile >= all) {
+            tile -= all;
+            continue;
         }
-        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(base + upto > tile);
-        if (beyond) {
-            const int at = __builtin_ctzll(beyond);
-            const int before = base + (at ? __builtin_amdgcn_readlane(upto, at - 1) : 0);
-            return {b0 + at, (tile - before) * BM, __builtin_amdgcn_readlane(r.x, at), __builtin_amdgcn_readlane(r.y, at),
-                    __builtin_amdgcn_readlane(len, at)};
+        int at, place;
+        if (by_height) {
+            const int cached = (int)((long long)max(0, min(len - r.y, p.a.max_pages * VF_TILE)) * p.group / BM), end = cached + tiles;
+            int low = 0, high = __builtin_amdgcn_readlane(lanes_upto(tiles ? end : 0, Max{}), 63), higher = 0;
+            while (high - low > 1) {   // the tile's height is low or more and less than high; `higher` tiles are at high or higher
+                const int middle = low + ((high - low) >> 1);
+                const int count = __builtin_amdgcn_readlane(lanes_upto(max(0, min(end - middle, tiles)), Plus{}), 63);
+                if (count > tile) low = middle;
+                else high = middle, higher = count;
+            }
+            const unsigned long long here = __builtin_amdgcn_ballot_w64(cached <= low && low < end);
+            const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(here >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)here, 0));
+            at = __builtin_ctzll(here & __builtin_amdgcn_ballot_w64(rank == tile - higher));
+            place = low - __builtin_amdgcn_readlane(cached, at);
+        } else {
+            at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > tile));
+            place = __builtin_amdgcn_readlane(upto, at) - 1 - tile;   // a sequence's last rows see the most
         }
-        base += __builtin_amdgcn_readlane(upto, 63);
+        return {b0 + at, place * BM, __builtin_amdgcn_readlane(r.x, at), __builtin_amdgcn_readlane(r.y, at), __builtin_amdgcn_readlane(len, at)};
     }
     return {0, 0, 0, 0, 0};
 }
@@ -123,7 +151,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
     const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int wave = any_wave % WAVES, kg = any_wave / WAVES, tid = threadIdx.x % (WAVES * 64);   // within the group of wavefronts kg
     const int rest = p.by_heads(blockIdx.x), kvh = blockIdx.x - rest * a.n_kv_heads, part = p.by_tiles(rest), place = rest - part * p.tiles;
-    const Tile t = find_tile<BM>(p, p.tiles - 1 - place);
+    const Tile t = find_tile<BM>(p, place, p.by_height);
     if (t.rows <= 0) return;
     const int group = p.group, n_items = t.rows * group, cap = min(t.kv_len, a.max_pages * VF_TILE);
     const int first_pos = t.kv_len - t.rows;                    // position of row 0
@@ -489,7 +517,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) VF_MFMA_KERNEL void attention_few_k
         t.rows = __builtin_amdgcn_readfirstlane(r.y);
         t.kv_len = __builtin_amdgcn_readfirstlane(p.kv_len[place]);
     } else {
-        t = find_tile<BM>(p, p.tiles - 1 - place);
+        t = find_tile<BM>(p, place, false);
         ids = p.table[(size_t)t.seq * a.table_stride + min(p_first + lane, a.max_pages - 1)];
     }
     const int32_t *table = p.table + (size_t)t.seq * a.table_stride;
@@ -863,6 +891,10 @@ int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const voi
     p.tiles = plan.tiles;
     p.tile_is_seq = plan.tile_is_seq;
     p.parts = plan.parts;
+    // Where workgroups meet on a CU, or wait for one, the long ones go first: twelve prompts of 230 to 2048 tokens at 0.5B 73 -> 69 us,
+    // six of 451 to 4096 at 1.5B 177 -> 169 us.  The search costs a workgroup up to 2 us (drafts of 16 sequences in parts,
+    // 276 workgroups: 23.5 -> 25.8 us), so calls that are split or have a workgroup a CU take the sequences as they come.
+    p.by_height = plan.kernel != FEW && plan.parts == 1 && p.a.n_seqs > 1 && (long long)plan.tiles * p.a.n_kv_heads > 256;
     p.part_pages = plan.part_pages;
     p.scale_log2e = (p.a.scale == 0.f ? 1.0f / sqrtf((float)p.a.head_dim) : p.a.scale) * 1.4426950408889634f;
     p.by_group = divisor(p.group);

@@ -260,6 +260,16 @@ def test_attention_many_sequences(dtype):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("sequences", [9, 70])
+@pytest.mark.parametrize("dtype,hkv", [("bf16", 2), ("f32", 7)])
+def test_attention_more_tiles_than_compute_units(dtype, hkv, sequences):
+    rng = np.random.default_rng(sequences)
+    rows = rng.integers(0, 7000 // sequences, sequences)
+    p = Packed([(int(m + rng.choice([0, 1, 90])), int(m)) for m in rows], 14, hkv, 64, dtype, seed=sequences)
+    assert sum(-(-int(m) * (14 // hkv) // 128) for m in rows) * hkv > 256
+    p.check(p.run())
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_attention_keys_a_row_does_not_see_add_nothing(dtype, rows):

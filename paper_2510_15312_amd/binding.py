@@ -523,6 +523,8 @@ def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, ma
     """q, out [rows, q heads, hd]; pool: one layer's pages; block_table int32 [n, pages]; row_off int32 [n + 1] and kv_len
     int32 [n] on the device; max_rows, max_keys: the host's bounds of a sequence's rows and keys."""
     args = _packed_args(q, pool, block_table, out, max_rows, max_keys, scale)
+    if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        _refuse("workspace: contiguous uint8 device tensor")
     _check(lib.vf_attention_packed(C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
                                    _ints("row_off", row_off, args.n_seqs + 1), _ints("kv_len", kv_len, args.n_seqs),
                                    out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(q)))

@@ -771,16 +771,16 @@ struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages; size_t bytes; }
 // What a call costs, in us: the way of the longest workgroup through its pages, what is more than the chip holds, and a merge.
 // The constants are fits to 176 calls (prompts, chunks behind a prefix, drafts and single tokens of 1 to 64 sequences in four
 // shapes, with every kernel and the numbers of parts below: profiles/packed_attention_plan_timings.txt); the choice costs 1.4 %
-// on average against the best of all (tiles of 128 items without parts throughout: 229 %), 14 % at most.
+// on average against the best of all (tiles of 128 items without parts throughout: 228 %), 14 % at most.
 struct KernelCost {
     float start, page, page_full;   // page: with up to half as many workgroups as the chip holds; page_full: with as many and more
     float more, more_start;         // for every further chip full: a page, a workgroup
 };
 struct TypeCost { KernelCost k[N_KERNELS]; float merge, merge_mb, merge8; };
 constexpr TypeCost COST[3] = {
-    {{{1.759f, 1.543f, 1.223f, 0.8654f, 1.002f}, {6.108f, 0.5364f, 0.6751f, 0.4049f, 2.977f}, {3.053f, 0.2486f, 0.4449f, 0.1005f, 2.478f}}, 3.832f, 0.4793f, 1.042f},   // bfloat16, heads of 64
-    {{{5.5f, 0.9f, 1.273f, 1.247f, 3.701f}, {6.783f, 0.8328f, 0.6975f, 0.6541f, 5.996f}, {4.43f, 0.3524f, 0.6176f, 0.199f, 3.766f}}, 4.463f, 0.4145f, 1.76f},   // bfloat16, heads of 128
-    {{{5.592f, 4.087f, 9.576f, 0.8124f, 2.904f}, {}, {5.655f, 0.6763f, 0.9135f, 1.002f, 1.447f}}, 2.728f, 0.9495f, 1.344f},   // float32
+    {{{4.399f, 1.083f, 1.279f, 1.006f, 0.001f}, {6.172f, 0.5866f, 0.7267f, 0.5461f, 1.187f}, {3.671f, 0.271f, 0.4648f, 0.101f, 2.197f}}, 3.019f, 0.5535f, 0.698f},   // bfloat16, heads of 64
+    {{{5.428f, 0.8914f, 1.3f, 0.8024f, 5.971f}, {7.131f, 0.8254f, 0.633f, 0.5692f, 10.61f}, {4.535f, 0.3585f, 0.6235f, 0.2623f, 2.653f}}, 4.267f, 0.4022f, 1.903f},   // bfloat16, heads of 128
+    {{{5.445f, 4.046f, 9.304f, 2.575f, 4.789f}, {}, {4.785f, 0.6812f, 0.8738f, 0.9143f, 1.732f}}, 3.535f, 0.6871f, 1.247f},   // float32
 };
 
 Plan make_plan(const vf_packed_args &a) {
@@ -809,6 +809,8 @@ Plan make_plan(const vf_packed_args &a) {
             float us = k.start + part_pages * (k.page + (k.page_full - k.page) * std::min(1.f, std::max(0.f, workgroups / half - 1.f))) +
                        std::max(0.f, workgroups / chip - 1.f) * (k.more * mean / used + k.more_start);
             if (parts > 1) us += cost.merge + cost.merge_mb * 4e-6f * a.total_rows * a.n_q_heads * used * (REC_HEAD + a.head_dim) + cost.merge8 * (((int)used - 1) / 8);
+            // less than the host takes for a call of one launch or two is not gained (one token behind 1024 at 0.5B in three parts 11.1 us, whole 8.0)
+            us = std::max(us, parts > 1 ? 11.f : 8.f) + 0.1f * us;
             if (best.parts && us >= best_cost) continue;
             best_cost = us;
             best = {kernel, tile_is_seq, 0, parts, part_pages, 0};

@@ -380,6 +380,39 @@ def test_packed_on_another_stream_and_in_a_graph():
             assert torch.equal(x, y)
 
 
+def test_the_binding_refuses_other_tensors():
+    """Types, shapes and strides that the C entry points cannot see."""
+    p = Packed([(70, 3), (5, 5)], 6, 2, 64, "bf16")
+    table, row_off, kv_len, out = i32(p.table), i32(p.row_off), i32(p.kv_len), torch.zeros_like(p.q)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+    good = dict(q=p.q, pool=p.pool, block_table=table, row_off=row_off, kv_len=kv_len, out=out, max_rows=5, max_keys=70, workspace=ws)
+    vf.vf_attention_packed(**good)
+    wrong = [("q", p.q.float()), ("q", p.q[:, :5]), ("q", p.q.cpu()), ("q", p.q.transpose(0, 1).contiguous().transpose(0, 1)),
+             ("pool", p.pool.float()), ("pool", p.pool[:, :1]), ("pool", p.pool.transpose(1, 2)), ("pool", p.pool.cpu()),
+             ("block_table", table.long()), ("block_table", table[0]), ("block_table", table.t()), ("block_table", table.cpu()),
+             ("row_off", row_off[:2]), ("row_off", row_off.long()), ("kv_len", kv_len[:1]), ("kv_len", i32([[1, 2], [3, 4]]).t()[0]),
+             ("out", out[:7]), ("out", out.float()), ("out", out[:, :, :32]), ("workspace", ws.float()),
+             ("workspace", ws[:1].expand(1 << 20)), ("workspace", ws.cpu())]
+    for name, value in wrong:
+        with pytest.raises(vf.VfError):
+            vf.vf_attention_packed(**{**good, name: value})
+    k, angles, pos, slot = p.q[:, :2], vf.vf_rotary_table(64, 1e4, 100), i32(range(8)), i32(range(8))
+    good = dict(q=p.q, k=k, v=k, table=angles, pos=pos, slot=slot, q_out=out, pool=p.pool)
+    vf.vf_rotary_append(**good)
+    for name, value in [("k", k.float()), ("v", k[:7]), ("v", p.q[:, :3]), ("table", angles.double()), ("table", angles[:, :, :1]),
+                        ("table", angles.transpose(0, 1)), ("pos", pos[:7]), ("slot", slot.long()), ("q_out", out.transpose(0, 1)),
+                        ("pool", p.pool[:, :, :, :64])]:
+        with pytest.raises(vf.VfError):
+            vf.vf_rotary_append(**{**good, name: value})
+    lens = dict(lens=i32([0]), new=i32([5]), free_pages=i32([0, 1]), n_free=i32([2]), block_table=i32([[-1, -1]]), row_off=i32([0, 0]),
+                pos=i32([0] * 5), slot=i32([0] * 5), kv_len=i32([0]), n_free_out=i32([0]))
+    vf.vf_pages_assign(**lens)
+    for name, value in [("lens", i32([])), ("new", lens["new"].long()), ("free_pages", lens["free_pages"].float()), ("n_free", i32([])),
+                        ("row_off", i32([0])), ("slot", i32([0] * 4)), ("kv_len", lens["kv_len"].cpu()), ("block_table", i32([-1]))]:
+        with pytest.raises(vf.VfError):
+            vf.vf_pages_assign(**{**lens, name: value})
+
+
 # ---- together with the rest of the framework ---------------------------------------------------
 
 @pytest.mark.parametrize("dtype", list(DTYPES))

@@ -768,19 +768,20 @@ int check(const char *name, const vf_packed_args *args) {
 enum { TILES = 0, TILES_TWO = 1, FEW = 2, N_KERNELS = 3 };   // 128 items a workgroup; the same, two groups of wavefronts; 16 items
 struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages; size_t bytes; };
 
-// What a call costs, in us: the way of the longest workgroup through its pages, what is more than the chip holds, and a merge.
-// The constants are fits to 176 calls (prompts, chunks behind a prefix, drafts and single tokens of 1 to 64 sequences in four
-// shapes, with every kernel and the numbers of parts below: profiles/packed_attention_plan_timings.txt); the choice costs 1.4 %
-// on average against the best of all (tiles of 128 items without parts throughout: 228 %), 14 % at most.
+// What a call costs, in us: the way of the longest workgroup through its pages or the chip's way through all of them, whichever is
+// longer, and a merge.  The constants are fits to 184 calls (prompts, chunks behind a prefix, drafts and single
+// tokens of 1 to 64 sequences in four shapes, with every kernel and the numbers of parts below:
+// profiles/packed_attention_plan_timings.txt); the choice costs 1.0 % on average against the best of all (tiles of 128 items
+// without parts throughout: 218 %), 13 % at most.
 struct KernelCost {
-    float start, page, page_full;   // page: with up to half as many workgroups as the chip holds; page_full: with as many and more
-    float more, more_start;         // for every further chip full: a page, a workgroup
+    float start, page, page_full;   // the longest way: with up to half as many workgroups as the chip holds, with as many and more
+    float load_page, load_start;    // a chip full of workgroups: a page, a workgroup
 };
 struct TypeCost { KernelCost k[N_KERNELS]; float merge, merge_mb, merge8; };
 constexpr TypeCost COST[3] = {
-    {{{4.399f, 1.083f, 1.279f, 1.006f, 0.001f}, {6.172f, 0.5866f, 0.7267f, 0.5461f, 1.187f}, {3.671f, 0.271f, 0.4648f, 0.101f, 2.197f}}, 3.019f, 0.5535f, 0.698f},   // bfloat16, heads of 64
-    {{{5.428f, 0.8914f, 1.3f, 0.8024f, 5.971f}, {7.131f, 0.8254f, 0.633f, 0.5692f, 10.61f}, {4.535f, 0.3585f, 0.6235f, 0.2623f, 2.653f}}, 4.267f, 0.4022f, 1.903f},   // bfloat16, heads of 128
-    {{{5.445f, 4.046f, 9.304f, 2.575f, 4.789f}, {}, {4.785f, 0.6812f, 0.8738f, 0.9143f, 1.732f}}, 3.535f, 0.6871f, 1.247f},   // float32
+    {{{0.001f, 1.291f, 1.171f, 1.034f, 0.834f}, {4.847f, 0.5623f, 0.581f, 0.5531f, 1.692f}, {0.5523f, 0.3306f, 0.1101f, 0.2405f, 2.32f}}, 5.793f, 0.4539f, 1.559f},   // bfloat16, heads of 64
+    {{{4.795f, 1.032f, 0.7804f, 0.8323f, 2.107f}, {6.637f, 0.9667f, 0.6065f, 0.525f, 2.013f}, {3.748f, 0.3978f, 0.3917f, 0.3569f, 2.231f}}, 4.369f, 0.6369f, 2.225f},   // bfloat16, heads of 128
+    {{{6.33f, 4.025f, 10.15f, 3.723f, 5.818f}, {}, {0.3175f, 1.075f, 0.7276f, 0.6559f, 4.85f}}, 3.913f, 0.6336f, 1.03f},   // float32
 };
 
 Plan make_plan(const vf_packed_args &a) {
@@ -805,12 +806,13 @@ Plan make_plan(const vf_packed_args &a) {
             const int part_pages = (pages + parts - 1) / parts;
             if ((pages + part_pages - 1) / part_pages != parts) continue;
             const float used = parts == 1 ? 1.f : std::min((float)parts, mean / part_pages + 1.f);
-            const float workgroups = groups * used, half = 0.5f * chip;
-            float us = k.start + part_pages * (k.page + (k.page_full - k.page) * std::min(1.f, std::max(0.f, workgroups / half - 1.f))) +
-                       std::max(0.f, workgroups / chip - 1.f) * (k.more * mean / used + k.more_start);
+            const float workgroups = groups * used;
+            const float crowd = std::min(1.f, std::max(0.f, 2 * workgroups / chip - 1.f));
+            const float way = part_pages * (k.page + (k.page_full - k.page) * crowd), load = workgroups / chip * (k.load_page * mean / used + k.load_start);
+            float us = k.start + std::max(way, load);
             if (parts > 1) us += cost.merge + cost.merge_mb * 4e-6f * a.total_rows * a.n_q_heads * used * (REC_HEAD + a.head_dim) + cost.merge8 * (((int)used - 1) / 8);
             // less than the host takes for a call of one launch or two is not gained (one token behind 1024 at 0.5B in three parts 11.1 us, whole 8.0)
-            us = std::max(us, parts > 1 ? 11.f : 8.f) + 0.1f * us;
+            us = std::max(us, parts > 1 ? 10.f : 8.f) + 0.1f * us;
             if (best.parts && us >= best_cost) continue;
             best_cost = us;
             best = {kernel, tile_is_seq, 0, parts, part_pages, 0};

@@ -120,12 +120,6 @@ __device__ __forceinline__ floatx16 mma(const Frag<float> &a, const Frag<float> 
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
     return c;
 }
-template <typename T> __device__ __forceinline__ bool any_not_finite(const Frag<T> &f) {
-    bool bad = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) bad |= not_finite(to_f32(f.v[j]));
-    return bad;
-}
 
 // Four kilobytes apart by OFF from memory straight to LDS, free to be moved by the compiler: a statement takes `order` and hands it on.
 // The destination goes through m0 (one idle cycle before the load); an instruction's own offset counts for both addresses.
@@ -141,8 +135,11 @@ template <int OFF> __device__ __forceinline__ int unit_to_lds(int order, const v
 // in bfloat16, half of one in float32 (the halves of a fragment's pieces in two units, so that a read of 16 bytes a lane
 // touches every bank once).  K rows are taken in the order that leaves a lane with eight consecutive keys per operand of
 // the second product: row m of a 32-key tile is key 16 (m >> 4) + 8 (m >> 2 & 1) + 4 (m >> 3 & 1) + (m & 3).
+// Heads of 64 in bfloat16 leave registers for a third wavefront on a SIMD, if a page's scores are not computed ahead of the page
+// before: three hide more than the order of one (twelve prompts of 230 to 2048 tokens at 0.5B 67 -> 60 us, one of 16384 570 -> 521 us).  Heads of 128 fill the registers of two.
+template <typename T, int HD, int KG> constexpr int tile_waves_per_simd = HD == 64 && KG == 1 && sizeof(T) == 2 ? 3 : 2;
 template <typename T, int HD, int KG>
-__global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kernel(PackedAttn p) {
+__global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, KG>)) void attention_tiles_kernel(PackedAttn p) {
     constexpr int WAVES = TILE_WAVES, BM = WAVES * 32, HALVES = sizeof(T) / 2, UNITS = HD / 4 * HALVES, LPW = UNITS / WAVES;   // units of a page
     constexpr int KD = HD / 32, KS = HD / 16, DB = HD / 32;
     static_assert(UNITS % (2 * WAVES) == 0, "a wavefront loads K or V");
@@ -295,42 +292,32 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = mma(v_piece(st, g / 2, g % 2, db), w[g], acc[db]);
     };
-    // The same where some keys are not seen by all items.  0 times a value that is not finite is not 0: if a key that only some
-    // items see holds such a value, every row takes the product with its own keys.
+    // The same where some keys are not seen by all items.  0 times a value that is not finite is not a number: where that comes
+    // out, every row takes the product with its own keys.
     auto products_masked = [&](const unsigned char *st, int t0) {
-        const int own = t0 + half * 8, page_last = min(wave_last, t0 + VF_TILE - 1);
+        const int page_last = min(wave_last, t0 + VF_TILE - 1);
         static_for<0, DB>([&](auto db) {
             constexpr int D = db;
-            // the largest exponents, of two bfloat16 values or one float32 value a word
-            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-            u16x2 top = {0, 0};
-            Frag<T> v[4];
+            floatx16 all = acc[D];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                v[g] = v_piece(st, g / 2, g % 2, D);
-                if constexpr (HALVES == 1) {
-                    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-                    const u32x4 x = __builtin_bit_cast(u32x4, v[g]);
+            for (int g = 0; g < 4; ++g) all = mma(v_piece(st, g / 2, g % 2, D), w[g], all);
+            bool bad = false;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[j] & 0x7fff7fffu));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) top = __builtin_elementwise_max(top, u16x2{(unsigned short)(__float_as_uint(v[g].v[j]) >> 16 & 0x7fff), 0});
-                }
-            }
-            if (!__builtin_amdgcn_ballot_w64(top[0] >= 0x7f80 || top[1] >= 0x7f80)) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) acc[D] = mma(v[g], w[g], acc[D]);
+            for (int i = 0; i < 16; i += 2) bad |= __builtin_isunordered(all[i], all[i + 1]);
+            if (!__builtin_amdgcn_ballot_w64(bad)) {
+                acc[D] = all;
             } else {
                 floatx16 sum = acc[D];   // of rows that see nothing here
                 for (int seen = max(wave_first, t0); seen <= page_last; ++seen) {
                     floatx16 c = acc[D];
+                    int keys = seen - t0 - half * 8;   // held back, or the compiler keeps 32 comparisons' operands through the whole kernel
+                    asm volatile("" : "+v"(keys));
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         Frag<T> x = v_piece(st, g / 2, g % 2, D);
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
-                            if (own + g * 16 + j > seen) x.v[j] = from_f32<T>(0.f);
+                            if (g * 16 + j > keys) x.v[j] = from_f32<T>(0.f);
                         c = mma(x, w[g], c);
                     }
                     if (min(last_key, t0 + VF_TILE - 1) == seen) sum = c;
@@ -384,7 +371,15 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
             }
         } else {
             int i = 0;
-            if (n_full > 0) {
+            if constexpr (tile_waves_per_simd<T, HD, KG> == 3) {
+                for (; i < n_full; ++i) {
+                    const Scores sc = scores(k_page(i));
+                    step(i);
+                    follow(sc);
+                    weights(sc);
+                    products(k_page(i));
+                }
+            } else if (n_full > 0) {
                 Scores even = scores(k_page(0)), odd;
                 follow(even);
                 auto last = [&](const Scores &sc) {
@@ -420,9 +415,10 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, 2) void attention_tiles_kerne
                 step(i);
                 tail(i);
                 if (!mine) continue;
+                const int keys = last_key - t0 - half * 8;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (t0 + half * 8 + (j >> 3) * 16 + (j & 7) > last_key) sc.t[j >> 4][j & 15] = -INFINITY;
+                    if ((j >> 3) * 16 + (j & 7) > keys) sc.t[j >> 4][j & 15] = -INFINITY;
                 follow(sc);
                 weights(sc);
                 products_masked(k_page(i), t0);
@@ -772,21 +768,22 @@ struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages; size_t bytes; }
 // longer, and a merge.  The constants are fits to 184 calls (prompts, chunks behind a prefix, drafts and single
 // tokens of 1 to 64 sequences in four shapes, with every kernel and the numbers of parts below:
 // profiles/packed_attention_plan_timings.txt); the choice costs 1.0 % on average against the best of all (tiles of 128 items
-// without parts throughout: 218 %), 13 % at most.
+// without parts throughout: 215 %), 13 % at most.
 struct KernelCost {
     float start, page, page_full;   // the longest way: with up to half as many workgroups as the chip holds, with as many and more
     float load_page, load_start;    // a chip full of workgroups: a page, a workgroup
 };
 struct TypeCost { KernelCost k[N_KERNELS]; float merge, merge_mb, merge8; };
 constexpr TypeCost COST[3] = {
-    {{{0.001f, 1.291f, 1.171f, 1.034f, 0.834f}, {4.847f, 0.5623f, 0.581f, 0.5531f, 1.692f}, {0.5523f, 0.3306f, 0.1101f, 0.2405f, 2.32f}}, 5.793f, 0.4539f, 1.559f},   // bfloat16, heads of 64
-    {{{4.795f, 1.032f, 0.7804f, 0.8323f, 2.107f}, {6.637f, 0.9667f, 0.6065f, 0.525f, 2.013f}, {3.748f, 0.3978f, 0.3917f, 0.3569f, 2.231f}}, 4.369f, 0.6369f, 2.225f},   // bfloat16, heads of 128
-    {{{6.33f, 4.025f, 10.15f, 3.723f, 5.818f}, {}, {0.3175f, 1.075f, 0.7276f, 0.6559f, 4.85f}}, 3.913f, 0.6336f, 1.03f},   // float32
+    {{{0.1096f, 1.141f, 1.316f, 1.328f, 0.001f}, {4.031f, 0.5942f, 0.5889f, 0.5321f, 1.727f}, {0.5085f, 0.3364f, 0.2482f, 0.2272f, 2.375f}}, 5.764f, 0.4402f, 1.466f},   // bfloat16, heads of 64
+    {{{4.853f, 1.057f, 0.8274f, 0.8943f, 1.981f}, {7.188f, 0.8256f, 0.6204f, 0.5674f, 1.125f}, {3.63f, 0.5332f, 0.3743f, 0.3209f, 3.417f}}, 5.142f, 0.5722f, 3.053f},   // bfloat16, heads of 128
+    {{{7.242f, 3.957f, 9.037f, 4.173f, 2.804f}, {}, {0.707f, 1.069f, 0.6218f, 0.5459f, 5.056f}}, 3.985f, 0.6412f, 0.9614f},   // float32
 };
 
 Plan make_plan(const vf_packed_args &a) {
     Plan best{};
-    const TypeCost &cost = COST[a.dtype == VF_F32 ? 2 : a.head_dim == 64 ? 0 : 1];
+    const int cost_of = a.dtype == VF_F32 ? 2 : a.head_dim == 64 ? 0 : 1;
+    const TypeCost &cost = COST[cost_of];
     const int group = a.n_q_heads / a.n_kv_heads, seqs = std::min(a.n_seqs, a.total_rows);
     const int pages = std::max(1, std::min(a.max_pages, (int)(((long long)a.max_keys + VF_TILE - 1) / VF_TILE)));
     const long long most_items = (long long)std::min(a.max_rows, a.total_rows) * group, items = (long long)a.total_rows * group;
@@ -798,7 +795,7 @@ Plan make_plan(const vf_packed_args &a) {
     for (int kernel = 0; kernel < N_KERNELS; ++kernel) {
         if (kernel == TILES_TWO && a.dtype == VF_F32) continue;   // one wavefront's float32 products fill a matrix unit
         if (kernel != FEW && most_items <= FEW_ITEMS) continue;     // every sequence one tile of 16: bound by memory, and more exact there
-        const int bm = kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32, chip = kernel == TILES ? 512 : 256;   // workgroups on 256 CUs
+        const int bm = kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32, chip = kernel != TILES ? 256 : cost_of == 0 ? 768 : 512;   // workgroups on 256 CUs
         const KernelCost &k = cost.k[kernel];
         const bool tile_is_seq = kernel == FEW && most_items <= bm;
         const float groups = (tile_is_seq ? seqs : items / (float)bm + (seqs > 1 ? 0.5f * seqs : 0.5f)) * a.n_kv_heads;

@@ -119,8 +119,8 @@ size_t vf_seq_state_bytes(const vf_model *m);
 
 /* Bytes of a KV pool.  page_tokens == 0: a private contiguous cache for `n` tokens (n is
  * rounded up to a multiple of 64 internally).  page_tokens == 64: a pool of `n` pages shared
- * by many sequences through their block tables.  Layout inside the pool is private to the
- * library (K row-major, V transposed in 64-token tiles); use vf_kv_read to inspect it. */
+ * by many sequences through their block tables.  Layer by layer, pages of 64 tokens in the layout that
+ * "packed batches over the page pool" below states; use vf_kv_read to inspect it. */
 size_t vf_kv_bytes(const vf_model *m, int page_tokens, int n);
 
 /* Binds a sequence to its KV memory.

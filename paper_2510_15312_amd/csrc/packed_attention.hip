@@ -146,10 +146,10 @@ template <int OFF> __device__ __forceinline__ int unit_to_lds(int order, const v
 //
 // What bounds it: a page of heads of 128 is 32 matrix instructions of 32 cycles among 135 on vectors and about 100 scalar and LDS
 // instructions of a wavefront, which issues one in four to five cycles; two wavefronts share a SIMD.  A prompt of 8192 tokens at 3B
-// (24 heads of 128, 8 of K and V) takes 380 to 390 us
-// = 1.06 to 1.08 PFLOP/s where a large matrix product reaches 1.3; the matrix units are busy 58 % of the cycles, at a clock that
+// (24 heads of 128, 8 of K and V) takes 373 to 394 us
+// = 1.05 to 1.1 PFLOP/s where a large matrix product reaches 1.3; the matrix units are busy 58 % of the cycles, at a clock that
 // the power limit has brought to 1.75 GHz.  20000 tokens at 1.5B: 1.12 PFLOP/s; at 0.5B (heads of 64, whose products are half as
-// long for the same softmax) 0.9.  Twelve prompts of 230 to 2048 tokens at 0.5B 60 us = 681 TFLOP/s: a tile has 16 pages on
+// long for the same softmax) 0.9.  Twelve prompts of 230 to 2048 tokens at 0.5B 59 us = 694 TFLOP/s: a tile has 16 pages on
 // average, of which the last one or two are masked, behind a start of three dependent reads.
 // Not taken, as no faster: three and four pages in flight, eight wavefronts on one page, a hand-laid order of the page's
 // instructions, the sum of the weights by additions instead of two-term products.
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
 // fragment of the pool is one contiguous kilobyte.  The wavefronts' sums meet in LDS.
 // Bound by bytes where there are enough sequences (32 tokens behind up to 8191 at 3B: 117 us = 5.0 TB/s, where a copy reaches 4.8; 64
 // behind up to 1999 at 1.5B 18.6 us = 3.8 TB/s), else by the launch and four dependent reads (lengths, page ids, keys, values): one token
-// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 8.3 us and 3.7 for the merge (2.5 TB/s in all).
+// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 8.4 us and 3 to 4 for the merge (2.6 TB/s in all).
 // 16 items leave half of a 16x16 product empty for groups of 6 to 8 heads, which costs nothing here; 32 a workgroup were no faster.
 // Operands of a 16x16 product over 32 values of k: 16 lanes each take 8.
 __device__ __forceinline__ floatx4 mma16(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx4 c) {
@@ -790,7 +790,7 @@ struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages, waves; size_t b
 // What a call costs, in us: the way of the longest workgroup through its pages or the chip's way through all of them, whichever is
 // longer, and a merge.  The constants are fits to 191 calls (prompts, chunks behind a prefix, drafts and single
 // tokens of 1 to 64 sequences in four shapes, with every kernel and the numbers of parts below:
-// profiles/packed_attention_plan_timings.txt); the choice costs 1.1 % on average against the best of all (tiles of 128 items
+// profiles/packed_attention_plan_timings.txt); the choice costs 0.9 % on average against the best of all (tiles of 128 items
 // without parts throughout: 223 %), 13 % at most.  What the kernels are to one another, in us: 2048 tokens at 1.5B 38 with 128 items, 33
 // with two groups, 57 with 16; six prompts of up to 4096 166, 188, 491; 22 rows behind 2000 in six parts 14.8, 15.6, 10.2, in one 36.8,
 // 31.6, 13.9; drafts of 16 sequences in eight parts 25, 22, 41.
@@ -802,7 +802,7 @@ struct TypeCost { KernelCost k[N_KERNELS + 1];   // the last: 16 items, four wav
                    float merge, merge_mb, merge8; };
 constexpr TypeCost COST[3] = {
     {{{2.991f, 1.12f, 1.167f, 1.143f, 0.001f}, {6.042f, 0.6525f, 0.5752f, 0.4454f, 3.089f}, {1.302f, 0.2779f, 0.3042f, 0.09254f, 1.694f}, {4.439f, 0.4318f, 0.43f, 0.4294f, 0.2164f}}, 5.297f, 0.4362f, 1.178f},   // bfloat16, heads of 64
-    {{{5.193f, 1.449f, 0.7045f, 0.8486f, 4.912f}, {6.45f, 0.7484f, 0.6672f, 0.4941f, 4.69f}, {2.515f, 0.4534f, 0.3162f, 0.2899f, 1.681f}, {3.932f, 0.7185f, 0.7905f, 0.6188f, 1.87f}}, 4.707f, 0.4452f, 2.016f},   // bfloat16, heads of 128
+    {{{4.291f, 0.9058f, 0.7355f, 0.7817f, 1.317f}, {5.425f, 0.8706f, 0.5725f, 0.4849f, 2.104f}, {3.007f, 0.4337f, 0.3039f, 0.281f, 1.466f}, {4.181f, 0.6562f, 0.7576f, 0.5794f, 1.727f}}, 4.363f, 0.6175f, 2.549f},   // bfloat16, heads of 128
     {{{2.321f, 5.142f, 7.635f, 1.674f, 0.5421f}, {}, {2.393f, 0.691f, 0.4236f, 0.622f, 0.001f}, {8.491f, 0.7689f, 1.807f, 1.221f, 1.31f}}, 4.161f, 1.255f, 0.001072f},   // float32
 };
 

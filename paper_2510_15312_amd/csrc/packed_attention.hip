@@ -785,6 +785,7 @@ int check(const char *name, const vf_packed_args *args) {
 // ---- choice of kernel and parts -------------------------------------------------------------------
 
 enum { TILES = 0, TILES_TWO = 1, FEW = 2, N_KERNELS = 3 };   // 128 items a workgroup; the same, two groups of wavefronts; 16 items
+constexpr int MAX_WORKGROUPS = 0x7fffff;   // of 512 threads, whose number stays below 2^32; tiles of 128 items and no parts never have more
 struct Plan { int kernel, tile_is_seq, tiles, parts, part_pages, waves; size_t bytes; };
 
 // What a call costs, in us: the way of the longest workgroup through its pages or the chip's way through all of them, whichever is
@@ -798,8 +799,10 @@ struct KernelCost {
     float start, page, page_full;   // the longest way: with up to half as many workgroups as the chip holds, with as many and more
     float load_page, load_start;    // a chip full of workgroups: a page, a workgroup
 };
-struct TypeCost { KernelCost k[N_KERNELS + 1];   // the last: 16 items, four wavefronts
-                   float merge, merge_mb, merge8; };
+struct TypeCost {
+    KernelCost k[N_KERNELS + 1];    // the last: 16 items, four wavefronts
+    float merge, merge_mb, merge8;
+};
 constexpr TypeCost COST[3] = {
     {{{2.991f, 1.12f, 1.167f, 1.143f, 0.001f}, {6.042f, 0.6525f, 0.5752f, 0.4454f, 3.089f}, {1.302f, 0.2779f, 0.3042f, 0.09254f, 1.694f}, {4.439f, 0.4318f, 0.43f, 0.4294f, 0.2164f}}, 5.297f, 0.4362f, 1.178f},   // bfloat16, heads of 64
     {{{4.291f, 0.9058f, 0.7355f, 0.7817f, 1.317f}, {5.425f, 0.8706f, 0.5725f, 0.4849f, 2.104f}, {3.007f, 0.4337f, 0.3039f, 0.281f, 1.466f}, {4.181f, 0.6562f, 0.7576f, 0.5794f, 1.727f}}, 4.363f, 0.6175f, 2.549f},   // bfloat16, heads of 128
@@ -823,10 +826,11 @@ Plan make_plan(const vf_packed_args &a) {
         if (kernel != FEW && most_items <= FEW_ITEMS) continue;     // every sequence one tile of 16: bound by memory, and more exact there
         const int bm = kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32;
         const bool tile_is_seq = kernel == FEW && most_items <= bm;
+        const long long tiles = tile_is_seq ? a.n_seqs : items / bm + seqs;   // a sequence ends in one tile that is not full
         const float groups = (tile_is_seq ? seqs : items / (float)bm + (seqs > 1 ? 0.5f * seqs : 0.5f)) * a.n_kv_heads;
         for (const int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
             const int part_pages = (pages + parts - 1) / parts;
-            if ((pages + part_pages - 1) / part_pages != parts) continue;
+            if ((pages + part_pages - 1) / part_pages != parts || tiles * parts * a.n_kv_heads > MAX_WORKGROUPS) continue;
             const float used = parts == 1 ? 1.f : std::min((float)parts, mean / part_pages + 1.f);
             const float workgroups = groups * used;
             // Tiles of 16 items: eight wavefronts share a tile's keys, or four where there are more tiles than compute units, of which one
@@ -843,11 +847,9 @@ Plan make_plan(const vf_packed_args &a) {
             us = std::max(us, parts > 1 ? 10.f : 8.f) + 0.1f * us;
             if (best.parts && us >= best_cost) continue;
             best_cost = us;
-            best = {kernel, tile_is_seq, 0, parts, part_pages, four ? 4 : 8, 0};
+            best = {kernel, tile_is_seq, (int)tiles, parts, part_pages, four ? 4 : 8, 0};
         }
     }
-    const int bm = best.kernel == FEW ? FEW_ITEMS : TILE_WAVES * 32;
-    best.tiles = best.tile_is_seq ? a.n_seqs : (int)(items / bm + seqs);   // a sequence ends in one tile that is not full
     if (best.parts > 1)
         best.bytes = (size_t)a.total_rows * a.n_q_heads * best.parts * (REC_HEAD + a.head_dim) * sizeof(float) + (size_t)a.total_rows * sizeof(int32_t);
     return best;
@@ -857,7 +859,7 @@ Plan make_plan(const vf_packed_args &a) {
 // eighth workgroup: with the parts of a tile next to one another some dies had the full ones and some the rest
 // (a prompt of 4096 tokens at 0.5B in two parts 70 us).
 template <typename F> int start(F kernel, long long blocks, int threads, int lds, const PackedAttn &p, hipStream_t st) {
-    if (blocks > 0x7fffff) return vf_fail(VF_ERR_UNSUPPORTED, "vf_attention_packed: %lld workgroups", blocks);
+    if (blocks > MAX_WORKGROUPS) return vf_fail(VF_ERR_UNSUPPORTED, "vf_attention_packed: %lld workgroups", blocks);
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), lds, st, p);
     VF_LAUNCH_CHECK("attention_packed");
     return VF_OK;

@@ -57,3 +57,13 @@ def test_single_tokens_take_the_kernel_of_sixteen_items():
     for rows in (1, 5, 400):
         for keys in (1, 64, 5000, 200000):
             assert _choice(_args("bf16", (16, 1, 128), (rows, rows, 1, keys)))[0] == 2
+
+
+def test_the_largest_calls_have_a_kernel():
+    """Tiles of 16 items would be more workgroups than a launch takes: 2^20 rows of 256 key heads."""
+    for dtype in ("bf16", "f32"):
+        for n, rows in ((1, 1 << 20), (4096, 1 << 20), (4096, 1 << 12)):
+            args = _args(dtype, (256, 256, 64), (n, rows, rows, rows))
+            kernel, parts = _choice(args)
+            tiles = rows // (16 if kernel == 2 else 128) + n
+            assert tiles * parts * 256 <= 0x7fffff

@@ -270,6 +270,15 @@ def test_attention_more_tiles_than_compute_units(dtype, hkv, sequences):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,hd,sequences,keys", [("bf16", 12, 2, 128, 150, 200), ("bf16", 24, 8, 128, 30, 1500), ("f32", 4, 4, 128, 70, 150),
+                                                            ("f32", 4, 4, 64, 40, 1200), ("bf16", 14, 2, 64, 150, 300)])
+def test_attention_more_single_tokens_than_compute_units(dtype, hq, hkv, hd, sequences, keys):
+    rng = np.random.default_rng(sequences)
+    p = Packed([(int(n), 1) for n in rng.integers(0, keys, sequences)], hq, hkv, hd, dtype, seed=sequences)
+    p.check(p.run())
+    p.check(p.run(max_keys=50 * keys))                        # in parts, wherever they end
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_attention_keys_a_row_does_not_see_add_nothing(dtype, rows):

@@ -548,8 +548,12 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
         const int last = min(first_pos + p.by_group(min(n_items - 1, item0 + BM - 1)), cap - 1);   // last key that an item sees
         const int pages = last < 0 ? 0 : last / VF_TILE + 1, parts = min(p.parts, (pages + p.part_pages - 1) / p.part_pages);
         const int p_end = part == p.parts - 1 ? pages : min(pages, p_first + p.part_pages);
-        if (p.parts > 1 && part == 0 && kvh == 0 && threadIdx.x < BM && item0 + (int)threadIdx.x < n_items)
-            p.used[row0 + p.by_group(item0 + threadIdx.x)] = parts;
+        if (p.parts > 1 && part == 0 && kvh == 0 && threadIdx.x < BM && item0 + (int)threadIdx.x < n_items) {
+            // Of a row whose heads lie in two tiles the first tile tells: the second has as many parts or more, of which the
+            // row sees no key past the first's, and which the heads of the first have no records of.
+            const int at = item0 + threadIdx.x, of = p.by_group(at);
+            if (at == of * group) p.used[row0 + of] = parts;
+        }
         if (p_first >= p_end && part > 0) continue;
         Frag<T> qf[KD];
         const int item = min(n_items - 1, item0 + l15), item_row = p.by_group(item), last_key = min(first_pos + item_row, cap - 1);

@@ -201,10 +201,11 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
     unsigned char *const pages_lds = smem + kg * (2 * UNITS * 1024);
     const unsigned lds0 = lds_address(pages_lds) + wave * (LPW * 1024);
     const int32_t *table = p.table + (size_t)t.seq * a.table_stride;
-    // ids of 64 pages, one per lane: those from ids_at on
+    // ids of 64 pages, one per lane: those from ids_at on.  The loads of K ask a step ahead of the products, so that a page asked
+    // for may also lie in front of them.
     int ids_at = p_begin, ids = table[min(p_begin + lane, a.max_pages - 1)];
     auto page_id = [&](int pg) {
-        if (pg - ids_at >= 64) {
+        if ((unsigned)(pg - ids_at) >= 64u) {
             ids_at = pg;
             ids = table[min(pg + lane, a.max_pages - 1)];
         }

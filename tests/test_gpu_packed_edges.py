@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import paper_2510_15312_amd as vf
-from test_gpu_packed import Packed
-from util_gpu import DEV
+from paper_2510_15312_amd.packed_batch import PackedBatch
+from test_gpu_packed import Packed, _pool_rows
+from util_gpu import DEV, i32
 
 pytestmark = pytest.mark.gpu
 TILES, TILES_TWO, FEW = 0, 1, 2     # kernels: 128 items a workgroup; the same with two groups of wavefronts; 16 items
@@ -75,3 +76,73 @@ def test_drafts_behind_1585_tokens():
     p = Packed([(1602, 17)], 12, 2, 128, "bf16", seed=19)
     assert plan(p) == (FEW, 6, 5)
     p.check(p.run())
+
+
+# ---- more than 64 pages in a part ------------------------------------------------------------------------------------
+
+def widen(p, pages):
+    p.table = np.pad(p.table, ((0, 0), (0, pages - p.table.shape[1])), constant_values=-1)
+    return p
+
+
+def check_around(p, out, b, position, present=None):
+    """Rows of sequence b in the tile of 128 items that holds a position: the tile's first, those around the position, the last."""
+    rows, group = int(p.row_off[b + 1] - p.row_off[b]), p.q.shape[1] // p.pool.shape[2]
+    first_pos = p.kv_len[b] - rows
+    tile = (position - first_pos) * group // 128
+    first, last = -(-tile * 128 // group), min(rows, (tile + 1) * 128 // group)
+    for a, z in ((first, first + 3), (position - first_pos - 1, position - first_pos + 2), (last - 2, last)):
+        check_rows(p, out, b, max(a, 0), min(z, rows), present)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd,kernel,seqs,width,max_keys", [
+    ("bf16", 12, 2, 128, TILES_TWO, [(5100, 5000)], 128, 5100), ("bf16", 14, 2, 64, TILES_TWO, [(5100, 5000)], 128, 5100),
+    ("bf16", 24, 8, 128, TILES, [(5100, 5000)], 128, 5100), ("bf16", 12, 2, 128, TILES, [(8300, 8100)], 256, 8300),
+    ("bf16", 14, 2, 64, TILES_TWO, [(8300, 8100)], 256, 8300),
+    ("bf16", 12, 2, 128, TILES_TWO, [(4200 - n % 3, 256) for n in range(15)] + [(4352, 256)], 128, 4352),
+    ("bf16", 14, 2, 64, TILES, [(4200, 900)] * 7 + [(4352, 900)], 70, 4352),
+    ("f32", 4, 4, 64, TILES, [(5100, 5000)], 128, 64), ("f32", 6, 2, 128, TILES, [(5100, 5000)], 128, 64)])   # in one part: the bound of keys is passed
+def test_chunks_that_cross_a_multiple_of_64_pages(dtype, hq, hkv, hd, kernel, seqs, width, max_keys):
+    """Tables wider than the sequences, -1 behind their pages."""
+    p = widen(Packed(seqs, hq, hkv, hd, dtype, seed=len(seqs)), width)
+    assert plan(p, None, max_keys)[:2] == (kernel, 1)
+    out = p.run(None, max_keys)
+    for b in {0, len(seqs) // 2, len(seqs) - 1}:
+        for position in range(4096, p.kv_len[b], 4096):
+            check_around(p, out, b, position)
+        check_rows(p, out, b, int(p.row_off[b + 1] - p.row_off[b]) - 2, int(p.row_off[b + 1] - p.row_off[b]))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd,kernel", [("bf16", 12, 2, 128, TILES), ("bf16", 14, 2, 64, TILES_TWO), ("f32", 4, 4, 64, TILES)])
+@pytest.mark.parametrize("missing", [[3], [62], [63], [64], [62, 63], [63, 128]])
+def test_missing_pages_among_more_than_64(missing, dtype, hq, hkv, hd, kernel):
+    """A page that is not there, in front of the 64th or there; entries 64 further on are pages."""
+    p = widen(Packed([(8300, 8100)], hq, hkv, hd, dtype, seed=63), 200)
+    max_keys = 64 if dtype == "f32" else 8300
+    assert plan(p, None, max_keys)[:2] == (kernel, 1)
+    p.table[0, missing] = -1
+    present = np.ones(8300, bool)
+    for page in missing:
+        present[page * 64:page * 64 + 64] = False
+    out = p.run(None, max_keys)
+    for position in (4095, 4160, 8192, 8290):
+        check_around(p, out, 0, position, present)
+
+
+def test_a_chunk_behind_a_chunk_of_a_batch():
+    """PackedBatch's tables are as wide as its requests may grow."""
+    hq, hkv, hd = 12, 2, 128
+    batch = PackedBatch(1, 1, hq, hkv, hd, pool_pages=100, max_tokens=8192, theta=1e4)
+    gen = torch.Generator(device=DEV).manual_seed(100)
+    for rows in (100, 5000):
+        row_off, pos = batch.begin([rows])
+        q, k, v = torch.randn((rows, hq + 2 * hkv, hd), generator=gen, device=DEV).to(torch.bfloat16).split((hq, hkv, hkv), 1)
+        out = batch.attend(0, q, k, v)
+        assert batch.finish() == [True]
+    p, t = Packed.__new__(Packed), np.arange(5100)
+    p.q = torch.empty_like(q.contiguous())
+    vf.vf_rotary_append(q, k, v, batch.angles, pos, torch.full_like(pos, -1), p.q, batch.pools[0])
+    slots = 64 * batch.table[0].cpu().numpy()[t // 64] + t % 64
+    p.hd, p.dt, p.pool, p.row_off, p.kv_len = hd, torch.bfloat16, batch.pools[0], np.array([0, 5000]), [5100]
+    p.k, p.v = ([x.double().cpu().numpy()] for x in _pool_rows(batch.pools[0], i32(slots), hd))
+    check_around(p, out, 0, 4096)

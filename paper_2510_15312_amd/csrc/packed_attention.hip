@@ -328,7 +328,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
                 acc[D] = all;
             } else {
                 floatx16 sum = acc[D];   // of rows that see nothing here
-                for (int seen = max(wave_first, t0); seen <= page_last; ++seen) {
+                for (int seen = min(max(wave_first, t0), page_last); seen <= page_last; ++seen) {   // (all rows may see the page whole)
                     floatx16 c = acc[D];
                     int keys = seen - t0 - half * 8;   // held back, or the compiler keeps 32 comparisons' operands through the whole kernel
                     asm volatile("" : "+v"(keys));

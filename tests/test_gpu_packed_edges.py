@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2510_15312_amd as vf
+from oracle import packed as op
 from paper_2510_15312_amd.packed_batch import PackedBatch
 from test_gpu_packed import Packed, _pool_rows
 from util_gpu import DEV, i32
@@ -25,14 +26,14 @@ def plan(p, max_rows=None, max_keys=None):
     return kernel.value, parts.value, -(-max(1, min(width, -(-max_keys // 64))) // parts.value)
 
 
-def check_rows(p, out, b, first, last, present=None):
+def check_rows(p, out, b, first, last, present=None, features=slice(None)):
     """Rows first .. last - 1 of sequence b against the oracle, as the last rows of a shorter sequence."""
     rows, n = int(p.row_off[b + 1] - p.row_off[b]), p.kv_len[b]
     end, at = n - (rows - last), slice(int(p.row_off[b]) + first, int(p.row_off[b]) + last)
     part = Packed.__new__(Packed)
     part.hd, part.dt, part.q, part.k, part.v = p.hd, p.dt, p.q[at], [p.k[b][:end]], [p.v[b][:end]]
     part.row_off, part.kv_len = np.array([0, last - first]), [end]
-    part.check(out[at], None if present is None else [present[:end]])
+    part.check(out[at], None if present is None else [present[:end]], rows=np.s_[:, :, features])
 
 
 # ---- records of a row whose heads lie in two tiles of 16 items -----------------------------------------------------
@@ -146,3 +147,37 @@ def test_a_chunk_behind_a_chunk_of_a_batch():
     p.hd, p.dt, p.pool, p.row_off, p.kv_len = hd, torch.bfloat16, batch.pools[0], np.array([0, 5000]), [5100]
     p.k, p.v = ([x.double().cpu().numpy()] for x in _pool_rows(batch.pools[0], i32(slots), hd))
     check_around(p, out, 0, 4096)
+
+
+# ---- values that are not finite -----------------------------------------------------------------------------------------
+
+MASKED = [("bf16", 4, 64, 1500, 64, TILES), ("bf16", 4, 128, 1500, 64, TILES), ("bf16", 2, 128, 3000, 3000, TILES_TWO), ("f32", 4, 64, 1500, 64, TILES)]
+
+
+@pytest.mark.parametrize("dtype,heads,hd,rows,max_keys,kernel", MASKED)
+def test_a_row_that_is_not_a_number_stays_alone(dtype, heads, hd, rows, max_keys, kernel):
+    """Rows 640 to 767 are a tile; those from 704 on see its first page, 640 to 703, whole."""
+    p = Packed([(rows, rows)], heads, heads, hd, dtype, seed=rows)
+    assert plan(p, None, max_keys)[0] == kernel
+    p.q[710] = float("nan")
+    out = p.run(None, max_keys)
+    assert out[710].isnan().all()
+    for first, last in ((640, 643), (670, 673), (700, 710), (711, 722), (733, 739), (765, 770)):
+        check_rows(p, out, 0, first, last)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,heads,hd,rows,max_keys,kernel", MASKED)
+def test_a_value_that_is_not_finite_stays_in_its_feature(dtype, heads, hd, rows, max_keys, kernel, value):
+    p = Packed([(rows, rows)], heads, heads, hd, dtype, seed=rows + 1)
+    assert plan(p, None, max_keys)[0] == kernel
+    key, feature = 645, 3
+    p.pool[int(p.table[0, key // 64]), 1, :, int(op.pool_place(hd)[1][key % 64, feature])] = value
+    p.v[0][key, :, feature] = 0                          # the oracle's value where nobody sees it
+    out = p.run(None, max_keys)
+    sees = torch.arange(rows, device=DEV) >= key
+    assert torch.isfinite(out[~sees]).all() and not torch.isfinite(out[sees][:, :, feature]).any()
+    out[:, :, feature] = torch.where(sees[:, None], 0, out[:, :, feature])
+    for first, last in ((640, 650), (700, 712), (760, 772), (830, 836)):
+        check_rows(p, out, 0, first, last, features=[i for i in range(hd) if i != feature])
+    check_rows(p, out, 0, 640, 645)

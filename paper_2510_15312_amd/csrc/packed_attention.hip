@@ -48,6 +48,7 @@ struct PackedAttn {
 };
 constexpr int REC_HEAD = 4;                    // maximum, sum, -, -
 constexpr int TILE_WAVES = 4, FEW_ITEMS = 16;
+constexpr float LOWEST = -1e30f;               // a running maximum of no keys
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -262,7 +263,11 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
-    float m_run = -1e30f, l_run = 0.f;   // l_run: this lane's keys
+    float m_run = LOWEST, l_run = 0.f;   // l_run: this lane's keys
+    // A weight's exponent is fma(score, by, -m_run), the scale inside.  m_run was rounded where the product of the fma is not, a
+    // common factor of up to 2^(2^-24 |m_run|): nothing up to 2^24.  Beyond that the scores are scaled and rounded first, and `by` is 1.
+    float by = p.scale_log2e;
+    bool far = false;
     struct Scores { floatx16 t[2]; };   // 32 keys each: register i of t[kt] is key 32 kt + 16 (i >> 3) + 8 half + (i & 7) of the page
     auto scores = [&](const unsigned char *st) {
         Scores sc;
@@ -278,7 +283,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
     };
     Frag<T> w[4];
     // The weights' common factor follows the maximum with slack: they stay below 2^8, and the sums are rescaled in few pages.
-    auto follow = [&](const Scores &sc) {
+    auto follow = [&](Scores &sc) {
         float mx = sc.t[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc.t[i >> 4][i & 15]);
@@ -289,12 +294,19 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] *= keep;
             m_run = m_new;
+            far = __builtin_amdgcn_ballot_w64(fabsf(m_new) > 0x1p24f && m_new != LOWEST);
+            by = far ? 1.f : p.scale_log2e;
+        }
+        if (far) {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sc.t[i >> 4][i & 15] *= p.scale_log2e;
         }
     };
     auto weights = [&](const Scores &sc) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(sc.t[i >> 4][i & 15], p.scale_log2e, -m_run));
+            const float x = __builtin_amdgcn_exp2f(fmaf(sc.t[i >> 4][i & 15], by, -m_run));
             if constexpr (HALVES == 2) l_run += x;
             w[i >> 3].v[i & 7] = from_f32<T>(x);
         }
@@ -393,7 +405,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
             int i = 0;
             if constexpr (tile_waves_per_simd<T, HD, KG> == 3) {
                 for (; i < n_full; ++i) {
-                    const Scores sc = scores(k_page(i));
+                    Scores sc = scores(k_page(i));
                     step(i);
                     follow(sc);
                     weights(sc);
@@ -562,7 +574,8 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
 #pragma unroll
         for (int kd = 0; kd < KD; ++kd) qf[kd] = load_frag<T>((const char *)(q + kd * 32));
         floatx4 acc[DB];
-        float m_run = -1e30f, l_run = 0.f;
+        float m_run = LOWEST, l_run = 0.f, by = p.scale_log2e;   // by, far: see attention_tiles_kernel
+        bool far = false;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
         // keys 32 i .. + 31, i = 2 p_first + wave, + WAVES ..
@@ -622,6 +635,13 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[db] *= keep;
                 m_run = m_new;
+                far = __builtin_amdgcn_ballot_w64(fabsf(m_new) > 0x1p24f && m_new != LOWEST);
+                by = far ? 1.f : p.scale_log2e;
+            }
+            if (far) {
+#pragma clang fp contract(off)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] *= p.scale_log2e;
             }
             load_k(i_next, id_next);
             // values of keys that nobody sees count as zeros; one that only some items see and that is not finite would reach
@@ -641,7 +661,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
             Frag<T> hi, lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[j], p.scale_log2e, -m_run));
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[j], by, -m_run));
                 l_run += w;
                 if constexpr (sizeof(T) == 2) {
                     const float top = __uint_as_float(__float_as_uint(w) & 0xffff0000u);
@@ -688,7 +708,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
         for (int j = threadIdx.x; j < BM * (HD / 4); j += WAVES * 64) {
             const int it = j / (HD / 4), d0 = j % (HD / 4) * 4, item = item0 + it;
             if (item >= n_items) break;
-            float M = -1e30f, L = 0.f;
+            float M = LOWEST, L = 0.f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) M = fmaxf(M, maxima[w * BM + it]);
             floatx4 o = {0.f, 0.f, 0.f, 0.f};
@@ -725,7 +745,7 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(PackedAttn p) {
     if (row >= a.total_rows) return;
     const bool inside = row >= p.row_off[0] && row < p.row_off[a.n_seqs];
     const float *rec = p.records + ((size_t)row * a.n_q_heads + head) * p.parts * REC;
-    float M = -1e30f, L = 0.f;
+    float M = LOWEST, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     // NR records are asked for together; how many there are is read first (asked for with all of a row's records, which spares
     // a round trip, many rows took up to a quarter longer for records that are not there, and few no less)

@@ -181,3 +181,34 @@ def test_a_value_that_is_not_finite_stays_in_its_feature(dtype, heads, hd, rows,
     for first, last in ((640, 650), (700, 712), (760, 772), (830, 836)):
         check_rows(p, out, 0, first, last, features=[i for i in range(hd) if i != feature])
     check_rows(p, out, 0, 640, 645)
+
+
+# ---- scores of any size -------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("low,high,signs", [(26, 40, (-1, 1))])
+@pytest.mark.parametrize("dtype,heads,hd,seq,max_keys,kernel,parts", [
+    ("bf16", 4, 64, (1500, 1500), 64, TILES, 1), ("bf16", 4, 128, (1500, 1500), 64, TILES, 1), ("bf16", 2, 128, (3000, 3000), 3000, TILES_TWO, 6),
+    ("f32", 4, 64, (1500, 1500), 64, TILES, 1), ("bf16", 4, 64, (300, 5), 300, FEW, 1), ("f32", 4, 128, (300, 5), 300, FEW, 1),
+    ("bf16", 4, 128, (2048, 3), 2048, FEW, 8)])
+def test_attention_of_scores_far_apart(dtype, heads, hd, seq, max_keys, kernel, parts, low, high, signs):
+    """Scores of 2^26 to 2^41 whose differences are 2^19 or more: a row's result is the mean of
+    the values of the keys with its highest score."""
+    p = Packed([seq], heads, heads, hd, dtype, seed=low)
+    assert plan(p, None, max_keys)[:2] == (kernel, parts)
+    n, rows = seq
+    rng = np.random.default_rng(high)
+    score = (rng.choice(signs, 40) * (1 + rng.integers(0, 128, 40) / 128) * 2.0 ** rng.integers(low, high, 40))[rng.integers(0, 40, n)]
+    p.q[:] = 0
+    p.q[:, :, 0] = 1
+    page, key = i32(p.table[0][np.arange(n) // 64]).long(), i32(np.arange(n) % 64).long()
+    for h in range(heads):
+        p.pool[page[:, None], 0, h, torch.as_tensor(op.pool_place(hd)[0], device=DEV)[key]] = 0
+        p.pool[page, 0, h, torch.as_tensor(op.pool_place(hd)[0][:, 0], device=DEV)[key]] = torch.as_tensor(score, device=DEV).to(p.dt)
+    out = p.run(None, max_keys, scale=1.0).double().cpu().numpy()
+    sees = np.arange(n) <= n - rows + np.arange(rows)[:, None]
+    highest = sees & (score == np.where(sees, score, -np.inf).max(1, keepdims=True))
+    weight = highest / highest.sum(1, keepdims=True)
+    want, spread = (np.einsum("rt,thd->rhd", weight, x) for x in (p.v[0], np.abs(p.v[0])))
+    # the weights are equal and their sums are exact up to rounding: n 2^-24 of the sum of sizes; bfloat16's weights and results 2^-8
+    unit = 2.0 ** -8 if dtype == "bf16" else 0.0
+    assert (np.abs(out - want) <= (n + 8) * 2.0 ** -23 * spread + unit * (spread + np.abs(want))).all()

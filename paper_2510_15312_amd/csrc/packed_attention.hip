@@ -48,7 +48,9 @@ struct PackedAttn {
 };
 constexpr int REC_HEAD = 4;                    // maximum, sum, -, -
 constexpr int TILE_WAVES = 4, FEW_ITEMS = 16;
-constexpr float LOWEST = -1e30f;               // a running maximum of no keys
+// A running maximum of no keys: the type's lowest, so that any score is above it, and 2^(LOWEST - m) is 0 beside any other m and 1
+// beside itself.
+constexpr float LOWEST = -3.40282347e38f;
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 

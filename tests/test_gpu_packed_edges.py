@@ -185,13 +185,13 @@ def test_a_value_that_is_not_finite_stays_in_its_feature(dtype, heads, hd, rows,
 
 # ---- scores of any size -------------------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("low,high,signs", [(26, 40, (-1, 1))])
+@pytest.mark.parametrize("low,high,signs", [(101, 120, (-1,)), (60, 100, (-1, 1)), (26, 40, (-1, 1))])
 @pytest.mark.parametrize("dtype,heads,hd,seq,max_keys,kernel,parts", [
     ("bf16", 4, 64, (1500, 1500), 64, TILES, 1), ("bf16", 4, 128, (1500, 1500), 64, TILES, 1), ("bf16", 2, 128, (3000, 3000), 3000, TILES_TWO, 6),
     ("f32", 4, 64, (1500, 1500), 64, TILES, 1), ("bf16", 4, 64, (300, 5), 300, FEW, 1), ("f32", 4, 128, (300, 5), 300, FEW, 1),
     ("bf16", 4, 128, (2048, 3), 2048, FEW, 8)])
 def test_attention_of_scores_far_apart(dtype, heads, hd, seq, max_keys, kernel, parts, low, high, signs):
-    """Scores of 2^26 to 2^41 whose differences are 2^19 or more: a row's result is the mean of
+    """Scores of 2^26 to 2^121 whose differences are 2^19 or more, all of them negative or not: a row's result is the mean of
     the values of the keys with its highest score."""
     p = Packed([seq], heads, heads, hd, dtype, seed=low)
     assert plan(p, None, max_keys)[:2] == (kernel, parts)

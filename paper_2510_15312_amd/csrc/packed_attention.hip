@@ -60,6 +60,8 @@ __device__ __forceinline__ int2 seq_rows(const PackedAttn &p, int b) {   // firs
     const int r0 = min(max(p.row_off[b], 0), p.a.total_rows), r1 = min(max(p.row_off[b + 1], r0), p.a.total_rows);
     return {r0, r1 - r0};
 }
+// Keys of a sequence, whatever the length holds: a negative one is none (the lowest would come out as the highest once rows are taken from it).
+__device__ __forceinline__ int seq_keys(const PackedAttn &p, int b) { return max(p.kv_len[b], 0); }
 // Over the wavefront's lanes, for values that are not negative: up to and with this lane.
 template <int CTRL, int ROWS, typename F> __device__ __forceinline__ int lane_step(int x, F f) {
     return f(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false));
@@ -82,7 +84,7 @@ template <int BM> __device__ __forceinline__ Tile find_tile(const PackedAttn &p,
     for (int b0 = 0; b0 < p.a.n_seqs; b0 += 64) {
         const int b = min(b0 + lane, p.a.n_seqs - 1);
         const int2 r = seq_rows(p, b);
-        const int len = p.kv_len[b];
+        const int len = seq_keys(p, b);
         const int tiles = b0 + lane < p.a.n_seqs ? (int)(((long long)r.y * p.group + BM - 1) / BM) : 0;
         const int upto = lanes_upto(tiles, Plus{}), all = __builtin_amdgcn_readlane(upto, 63);
         if (tile >= all) {
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(WAVES * 64) VF_MFMA_KERNEL void attention_few_kerne
         const int2 r = seq_rows(p, place);
         t.row0 = __builtin_amdgcn_readfirstlane(r.x);
         t.rows = __builtin_amdgcn_readfirstlane(r.y);
-        t.kv_len = __builtin_amdgcn_readfirstlane(p.kv_len[place]);
+        t.kv_len = __builtin_amdgcn_readfirstlane(seq_keys(p, place));
     } else {
         t = find_tile<BM>(p, place, false);
         ids = p.table[(size_t)t.seq * a.table_stride + min(p_first + lane, a.max_pages - 1)];

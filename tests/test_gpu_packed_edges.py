@@ -212,3 +212,20 @@ def test_attention_of_scores_far_apart(dtype, heads, hd, seq, max_keys, kernel, 
     # the weights are equal and their sums are exact up to rounding: n 2^-24 of the sum of sizes; bfloat16's weights and results 2^-8
     unit = 2.0 ** -8 if dtype == "bf16" else 0.0
     assert (np.abs(out - want) <= (n + 8) * 2.0 ** -23 * spread + unit * (spread + np.abs(want))).all()
+
+
+# ---- lengths that are none ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd,rows,max_keys,kernel", [
+    ("bf16", 4, 4, 64, 1500, 64, TILES), ("bf16", 12, 2, 128, 1500, 64, TILES), ("bf16", 12, 2, 128, 300, 2560, TILES_TWO), ("f32", 4, 4, 64, 1500, 64, TILES),
+    ("bf16", 12, 2, 128, 2, 64, FEW), ("bf16", 12, 2, 128, 2, 5000, FEW), ("f32", 4, 2, 64, 9, 64, FEW)])
+def test_attention_of_negative_lengths(dtype, hq, hkv, hd, rows, max_keys, kernel):
+    """Down to the lowest: rows that see nothing, beside a sequence that stands."""
+    p = widen(Packed([(64, rows), (64, rows), (100, min(rows, 100)), (64, rows)], hq, hkv, hd, dtype, seed=64), 40)
+    assert plan(p, rows, max_keys)[0] == kernel
+    p.kv_len = [-2 ** 31, -1, 100, -2 ** 31 + rows]
+    out = p.run(rows, max_keys)
+    a, z = int(p.row_off[2]), int(p.row_off[3])
+    assert not out[:a].any() and not out[z:].any()
+    check_rows(p, out, 2, 0, min(3, z - a))
+    check_rows(p, out, 2, max(0, z - a - 3), z - a)

@@ -76,6 +76,15 @@ template <typename F> __device__ __forceinline__ int lanes_upto(int x, F f) {
 }
 struct Plus { __device__ __forceinline__ int operator()(int x, int y) const { return x + y; } };
 struct Max { __device__ __forceinline__ int operator()(int x, int y) const { return max(x, y); } };
+// Tiles of cached tokens.  Past 2^30 the order of heights does not matter, but that no height overflows does: a tile that the search
+// does not find would lie outside its sequence.
+__host__ __device__ constexpr int cached_tiles(int tokens, int group, int bm) {
+    const long long tiles = (long long)(tokens > 0 ? tokens : 0) * group / bm;
+    return tiles < (1 << 30) ? (int)tiles : 1 << 30;
+}
+static_assert(cached_tiles(0x7fffffff / VF_TILE * VF_TILE, 256, TILE_WAVES * 32) + (long long)VF_PACKED_MAX_ROWS * 256 / (TILE_WAVES * 32) <= 0x7fffffff &&
+                  cached_tiles(0x7fffffff, 256, TILE_WAVES * 32) > 0 && cached_tiles(8192, 3, TILE_WAVES * 32) == 192 && cached_tiles(-5, 3, 128) == 0,
+              "the longest sequence of the largest group");
 // Tile number `tile` of all, 64 sequences at a time: sequence by sequence, or those with the most keys first (by_height).  A tile's
 // height is its place in its sequence, counted in tiles, cached tokens among them; as high as h or higher are clamp(end - h, 0, tiles)
 // of a sequence.
@@ -93,7 +102,7 @@ template <int BM> __device__ __forceinline__ Tile find_tile(const PackedAttn &p,
         }
         int at, place;
         if (by_height) {
-            const int cached = (int)((long long)max(0, min(len - r.y, p.a.max_pages * VF_TILE)) * p.group / BM), end = cached + tiles;
+            const int cached = cached_tiles(min(len - r.y, p.a.max_pages * VF_TILE), p.group, BM), end = cached + tiles;
             int low = 0, high = __builtin_amdgcn_readlane(lanes_upto(tiles ? end : 0, Max{}), 63), higher = 0;
             while (high - low > 1) {   // the tile's height is low or more and less than high; `higher` tiles are at high or higher
                 const int middle = low + ((high - low) >> 1);

@@ -31,6 +31,8 @@ class PackedBatch:
 
     def begin(self, new):
         """new[b] tokens for request b.  Returns the device's row offsets [n + 1] and the rows' positions (-1: refused)."""
+        if len(new) != len(self.host_lens):
+            raise ValueError(f"{len(new)} numbers of tokens for {len(self.host_lens)} requests")
         self.new, rows = [int(w) for w in new], sum(max(0, int(w)) for w in new)
         self.pos = torch.empty(rows, dtype=torch.int32, device=self.device)
         self.slot = torch.empty_like(self.pos)

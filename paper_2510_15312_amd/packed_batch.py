@@ -28,9 +28,16 @@ class PackedBatch:
         self.n_free, self.n_free_after = ints(1, value=pool_pages), ints(1)
         self.lens, self.row_off, self.kv_len = ints(n_requests), ints(n_requests + 1), ints(n_requests)
         self.host_lens, self.host_free = [0] * n_requests, pool_pages
+        self.in_step = False
+
+    def _within(self, step, what):
+        if self.in_step is not step:
+            raise RuntimeError(f"{what} within a step" if self.in_step else f"{what} without a step")
 
     def begin(self, new):
-        """new[b] tokens for request b.  Returns the device's row offsets [n + 1] and the rows' positions (-1: refused)."""
+        """new[b] tokens for request b.  Returns the device's row offsets [n + 1] and the rows' positions (-1: refused).  A step that
+        was begun and not finished is given up."""
+        self.in_step = False
         if len(new) != len(self.host_lens):
             raise ValueError(f"{len(new)} numbers of tokens for {len(self.host_lens)} requests")
         self.new, rows = [int(w) for w in new], sum(max(0, int(w)) for w in new)
@@ -40,11 +47,13 @@ class PackedBatch:
                            self.table, self.row_off, self.pos, self.slot, self.kv_len, self.n_free_after)
         self.workspace, self.max_rows = None, max([0] + self.new)
         self.max_keys = max(h + max(0, w) for h, w in zip(self.host_lens, self.new))
+        self.in_step = True
         return self.row_off, self.pos
 
     def attend(self, layer, q, k, v):
         """q [rows, q heads, head_dim], k, v [rows, kv heads, head_dim] before rotation (views of one wider matrix allowed): stores
         k and v, returns the attention of every row, zeros for the rows of a refused request."""
+        self._within(True, "attend")
         pool, rotated, out = self.pools[layer], q.new_empty(q.shape), q.new_empty(q.shape)
         vf.vf_rotary_append(q, k, v, self.angles, self.pos, self.slot, rotated, pool, self.pairs)
         if self.workspace is None:      # the layers of a step share it
@@ -55,6 +64,8 @@ class PackedBatch:
     def finish(self):
         """Ends the step: the lengths move on, the free list is what is left.  Returns a truth value per request: False where
         the pool or the table had no room, so that the request stands as before and may ask again."""
+        self._within(True, "finish")
+        self.in_step = False
         self.lens = torch.where(self.kv_len > 0, self.kv_len, self.lens)
         self.n_free, self.n_free_after = self.n_free_after, self.n_free
         *lens, self.host_free = torch.cat([self.kv_len, self.n_free]).tolist()
@@ -63,7 +74,9 @@ class PackedBatch:
         return granted
 
     def keep(self, request, tokens):
-        """Of the request's tokens the first `tokens` stay (drafts that were not accepted go); pages behind them are free again."""
+        """Of the request's tokens the first `tokens` stay (drafts that were not accepted go); pages behind them are free again.
+        Between steps: a step that is open has taken its pages from the free list as it stood."""
+        self._within(False, "keep")
         first, last = -(-tokens // PAGE), -(-self.host_lens[request] // PAGE)
         if not 0 <= tokens <= self.host_lens[request]:
             raise ValueError(f"request {request} holds {self.host_lens[request]} tokens, not {tokens}")
@@ -76,5 +89,5 @@ class PackedBatch:
         self.host_lens[request] = tokens
 
     def release(self, request):
-        """The request is over: its place in the batch and its pages are free."""
+        """The request is over: its place in the batch and its pages are free.  Between steps, as `keep`."""
         self.keep(request, 0)

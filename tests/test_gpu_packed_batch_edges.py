@@ -35,3 +35,46 @@ def test_begin_takes_a_number_for_every_request(new):
     with pytest.raises(ValueError):
         batch.begin(new)
     assert step(batch, [70, 0, 1]) == [True] * 3 and pages_of(batch) == list(range(8))
+
+
+def test_pages_are_not_given_back_within_a_step():
+    batch = make()
+    step(batch, [130, 64, 1])
+    batch.begin([1, 1, 1])
+    for call in (lambda: batch.keep(0, 5), lambda: batch.release(1)):
+        with pytest.raises(RuntimeError):
+            call()
+    batch.attend(0, *rows_of(3))
+    assert batch.finish() == [True] * 3
+    assert batch.host_lens == [131, 65, 2] and pages_of(batch) == list(range(8)) and batch.host_free == 2
+    batch.release(1)
+    assert batch.host_lens == [131, 0, 2] and pages_of(batch) == list(range(8)) and batch.host_free == 4
+    assert step(batch, [0, 256, 0]) == [True] * 3 and pages_of(batch) == list(range(8)) and batch.host_free == 0
+
+
+def test_a_step_is_finished_once():
+    batch = make()
+    for call in (batch.finish, lambda: batch.attend(0, *rows_of(1))):     # no step yet
+        with pytest.raises(RuntimeError):
+            call()
+    step(batch, [130, 64, 1])
+    for call in (batch.finish, lambda: batch.attend(0, *rows_of(195))):   # the step is over
+        with pytest.raises(RuntimeError):
+            call()
+    assert step(batch, [63, 65, 0]) == [True] * 3 and batch.host_lens == [193, 129, 1]
+    assert pages_of(batch) == list(range(8)) and batch.host_free == 0
+
+
+def test_a_step_may_begin_again():
+    """The step before was given up: nothing of it stays."""
+    batch = make()
+    step(batch, [60, 0, 0])
+    batch.begin([100, 100, 100])
+    assert step(batch, [10, 64, 0]) == [True] * 3 and batch.host_lens == [70, 64, 0] and pages_of(batch) == list(range(8))
+    batch.begin([100, 100, 100])
+    with pytest.raises(ValueError):
+        batch.begin([1])
+    with pytest.raises(RuntimeError):                                     # no step is open
+        batch.finish()
+    batch.release(0)
+    assert step(batch, [0, 1, 300]) == [True, True, False] and pages_of(batch) == list(range(8)) and batch.host_free == 6

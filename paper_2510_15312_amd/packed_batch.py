@@ -43,7 +43,9 @@ class PackedBatch:
         self.new, rows = [int(w) for w in new], sum(max(0, int(w)) for w in new)
         self.pos = torch.empty(rows, dtype=torch.int32, device=self.device)
         self.slot = torch.empty_like(self.pos)
-        vf.vf_pages_assign(self.lens, torch.tensor(self.new, dtype=torch.int32, device=self.device), self.free, self.n_free,
+        # from pinned memory, whose copy nobody waits for; torch keeps the memory until the copy is done
+        new_dev = torch.tensor(self.new, dtype=torch.int32, pin_memory=True).to(self.device, non_blocking=True)
+        vf.vf_pages_assign(self.lens, new_dev, self.free, self.n_free,
                            self.table, self.row_off, self.pos, self.slot, self.kv_len, self.n_free_after)
         self.workspace, self.max_rows = None, max([0] + self.new)
         self.max_keys = max(h + max(0, w) for h, w in zip(self.host_lens, self.new))

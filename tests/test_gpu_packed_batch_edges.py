@@ -78,3 +78,30 @@ def test_a_step_may_begin_again():
         batch.finish()
     batch.release(0)
     assert step(batch, [0, 1, 300]) == [True, True, False] and pages_of(batch) == list(range(8)) and batch.host_free == 6
+
+
+def test_a_step_waits_for_the_device_once():
+    """Nothing from begin to finish's copy waits, whatever is still running."""
+    batch = make()
+    step(batch, [130, 0, 1])
+    step(batch, [1, 64, 1])                               # memory and kernels of such a step are there
+    rows, before = rows_of(3), torch.cuda.get_sync_debug_mode()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        batch.begin([1, 1, 1])
+        batch.attend(0, *rows)
+    finally:
+        torch.cuda.set_sync_debug_mode(before)
+    assert batch.finish() == [True] * 3 and batch.host_lens == [132, 65, 3]
+
+
+def test_numbers_of_tokens_are_those_of_their_begin():
+    """Steps given up one after the other, faster than the device takes them: each has its own numbers on their way."""
+    batch = make()
+    torch.cuda._sleep(20_000_000)
+    for i in range(200):
+        batch.begin([i % 7, 1 + i % 64, 3])
+    batch.begin([130, 5, 64])
+    batch.attend(0, *rows_of(199))
+    assert batch.row_off.tolist() == [0, 130, 135, 199]
+    assert batch.finish() == [True] * 3 and batch.host_lens == [130, 5, 64] and pages_of(batch) == list(range(8))

@@ -48,7 +48,7 @@ class PackedBatch:
         vf.vf_pages_assign(self.lens, new_dev, self.free, self.n_free,
                            self.table, self.row_off, self.pos, self.slot, self.kv_len, self.n_free_after)
         self.workspace, self.max_rows = None, max([0] + self.new)
-        self.max_keys = max(h + max(0, w) for h, w in zip(self.host_lens, self.new))
+        self.max_keys = max([0] + [h + w for h, w in zip(self.host_lens, self.new) if w > 0])
         self.in_step = True
         return self.row_off, self.pos
 

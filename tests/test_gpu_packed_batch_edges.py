@@ -105,3 +105,14 @@ def test_numbers_of_tokens_are_those_of_their_begin():
     batch.attend(0, *rows_of(199))
     assert batch.row_off.tolist() == [0, 130, 135, 199]
     assert batch.finish() == [True] * 3 and batch.host_lens == [130, 5, 64] and pages_of(batch) == list(range(8))
+
+
+def test_bounds_are_those_of_the_requests_in_the_step():
+    """A long request without tokens in the step does not choose the others' kernel and parts."""
+    batch = make(requests=3, pages=40, tokens=2048)
+    step(batch, [2000, 10, 0])
+    for new, rows, keys in (([0, 1, 0], 1, 11), ([0, 3, 70], 70, 70), ([1, 0, 0], 1, 2001), ([0, 0, 0], 0, 0), ([0, -4, 2], 2, 72)):
+        batch.begin(new)
+        assert (batch.max_rows, batch.max_keys) == (rows, keys)
+        batch.attend(0, *rows_of(sum(max(0, w) for w in new)))
+        assert batch.finish() == [w >= 0 for w in new]

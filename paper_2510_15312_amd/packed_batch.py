@@ -3,7 +3,7 @@
 A step gives every request some more tokens (a whole prompt, a chunk of one, drafts, one token, none), packed row behind row.
 `begin` takes their pages from the free list (`vf_pages_assign`), `attend` stores a layer's keys and values and attends over the
 cache (`vf_rotary_append`, `vf_attention_packed`), `finish` tells which requests had room: one copy of a few integers, the
-step's one synchronisation.  `keep` takes back tokens that were not accepted, `release` gives a request's pages back.
+step's one synchronisation.  All of them work on the current stream; where it changes, the caller lets the next wait for the last.  `keep` takes back tokens that were not accepted, `release` gives a request's pages back.
 The projections around `attend`, the norms and the feed-forward are the caller's.
 """
 import torch
@@ -42,7 +42,7 @@ class PackedBatch:
             raise ValueError(f"{len(new)} numbers of tokens for {len(self.host_lens)} requests")
         self.new, rows = [int(w) for w in new], sum(max(0, int(w)) for w in new)
         self.pos = torch.empty(rows, dtype=torch.int32, device=self.device)
-        self.slot = torch.empty_like(self.pos)
+        self.slot, self.stream = torch.empty_like(self.pos), vf._stream_of(self.pos)
         # from pinned memory, whose copy nobody waits for; torch keeps the memory until the copy is done
         new_dev = torch.tensor(self.new, dtype=torch.int32, pin_memory=True).to(self.device, non_blocking=True)
         vf.vf_pages_assign(self.lens, new_dev, self.free, self.n_free,
@@ -58,8 +58,15 @@ class PackedBatch:
         self._within(True, "attend")
         pool, rotated, out = self.pools[layer], q.new_empty(q.shape), q.new_empty(q.shape)
         vf.vf_rotary_append(q, k, v, self.angles, self.pos, self.slot, rotated, pool, self.pairs)
+        stream = vf._stream_of(q)
+        if stream != self.stream:       # another than begin's
+            self.pos.record_stream(torch.cuda.current_stream(self.device))
+            self.slot.record_stream(torch.cuda.current_stream(self.device))
         if self.workspace is None:      # the layers of a step share it
             self.workspace = vf.vf_attention_packed_workspace(rotated, pool, self.table, self.max_rows, self.max_keys)
+            self.workspace_stream = stream
+        elif stream != self.workspace_stream:
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))
         vf.vf_attention_packed(rotated, pool, self.table, self.row_off, self.kv_len, out, self.max_rows, self.max_keys, self.workspace)
         return out
 
@@ -68,7 +75,7 @@ class PackedBatch:
         the pool or the table had no room, so that the request stands as before and may ask again."""
         self._within(True, "finish")
         self.in_step = False
-        self.lens = torch.where(self.kv_len > 0, self.kv_len, self.lens)
+        torch.where(self.kv_len > 0, self.kv_len, self.lens, out=self.lens)
         self.n_free, self.n_free_after = self.n_free_after, self.n_free
         *lens, self.host_free = torch.cat([self.kv_len, self.n_free]).tolist()
         granted = [length > 0 or w == 0 for length, w in zip(lens, self.new)]

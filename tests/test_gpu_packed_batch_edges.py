@@ -116,3 +116,34 @@ def test_bounds_are_those_of_the_requests_in_the_step():
         assert (batch.max_rows, batch.max_keys) == (rows, keys)
         batch.attend(0, *rows_of(sum(max(0, w) for w in new)))
         assert batch.finish() == [w >= 0 for w in new]
+
+
+def test_memory_of_a_step_waits_for_the_streams_that_use_it():
+    """begin on one stream, a first attend on another, a second on a third: what they share is not handed out again before
+    they are done with it."""
+    batch = make(requests=2, pages=40, tokens=2048)
+    step(batch, [2000, 10])
+    rows, main = rows_of(2), torch.cuda.current_stream()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    batch.begin([1, 1])
+    for before, stream in ((main, one), (one, two)):
+        stream.wait_stream(before)
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(20_000_000)
+            batch.attend(0, *rows)
+
+    def given_again(name, stream):
+        """Whether memory of a tensor that the batch lets go is given to others at once."""
+        t = getattr(batch, name)
+        shape, dtype, first, last = t.shape, t.dtype, t.data_ptr(), t.data_ptr() + t.nbytes
+        del t
+        setattr(batch, name, None)
+        with torch.cuda.stream(stream):
+            held = [torch.empty(shape, dtype=dtype, device=DEV) for _ in range(64)]     # (never written)
+        return any(x.data_ptr() < last and first < x.data_ptr() + x.nbytes for x in held)
+    assert batch.workspace.numel() > 0
+    again = [given_again("workspace", one), given_again("pos", main), given_again("slot", main)]
+    lens = batch.lens.data_ptr()
+    main.wait_stream(two)
+    assert batch.finish() == [True] * 2 and batch.lens.tolist() == [2001, 11]
+    assert again == [False] * 3 and batch.lens.data_ptr() == lens

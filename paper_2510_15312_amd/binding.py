@@ -6,6 +6,7 @@ in the library's kernels.  There is no fallback: if the library is missing the
 import fails.
 """
 import ctypes as C
+import functools
 import os
 
 import torch  # first: brings the HIP runtime the library links against into the process
@@ -415,35 +416,52 @@ def _refuse(what):
 _I32 = torch.int32
 
 
-def _ints(name, t, n):
+@functools.cache
+def _several_devices():
+    return torch.cuda.device_count() > 1
+
+
+def _device(name, t):
+    """The number of a tensor's device, on which all others of the call have to be; None where there is one device only, so that
+    `is_cuda` says the same (asking every tensor of a call for its number takes 0.5 us of the call's 8)."""
+    if not t.is_cuda:
+        _refuse(f"{name}: device tensor")
+    return t.get_device() if _several_devices() else None
+
+
+def _on(device):
+    return " on the device" if device is None else f" on device {device}"
+
+
+def _ints(name, t, n, device):
     """The address of an int32 device tensor of at least n entries one behind the other."""
-    if t.dtype is not _I32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
-        _refuse(f"{name}: contiguous int32 device tensor of {n} entries")
+    if t.dtype is not _I32 or not t.is_cuda or t.numel() < n or not t.is_contiguous() or device is not None and t.get_device() != device:
+        _refuse(f"{name}: contiguous int32 tensor of {n} entries{_on(device)}")
     return t.data_ptr()
 
 
-def _rows(name, t, dtype, rows, heads, hd):
+def _rows(name, t, dtype, rows, heads, hd, device):
     """The row stride of a device tensor [rows, heads, hd] whose rows are contiguous."""
-    if t.dtype is not dtype or t.shape != (rows, heads, hd) or not t.is_cuda:
-        _refuse(f"{name}: device tensor [{rows}, {heads}, {hd}] of {dtype}")
+    if t.dtype is not dtype or t.shape != (rows, heads, hd) or not t.is_cuda or device is not None and t.get_device() != device:
+        _refuse(f"{name}: tensor [{rows}, {heads}, {hd}] of {dtype}{_on(device)}")
     row, head, one = t.stride()
     if one != 1 or (heads > 1 and head != hd):
         _refuse(f"{name}: rows that are contiguous")
     return row if rows > 1 else max(row, heads * hd)
 
 
-def _pool(t, hd, dtype):
+def _pool(t, hd, dtype, device):
     """(pages, kv heads) of one layer's pages, [pages, 2, kv heads, 64 * hd]."""
     s = t.shape
-    if len(s) != 4 or s[1] != 2 or s[3] != 64 * hd or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda:
-        _refuse(f"pool: contiguous device tensor [pages, 2, kv heads, {64 * hd}] of {dtype}")
+    if len(s) != 4 or s[1] != 2 or s[3] != 64 * hd or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or device is not None and t.get_device() != device:
+        _refuse(f"pool: contiguous tensor [pages, 2, kv heads, {64 * hd}] of {dtype}{_on(device)}")
     return s[0], s[2]
 
 
-def _table(t):
+def _table(t, device):
     """(sequences, entries a sequence, stride) of a block table."""
-    if t.dim() != 2 or t.dtype is not _I32 or not t.is_cuda:
-        _refuse("block table: int32 device tensor [sequences, pages]")
+    if t.dim() != 2 or t.dtype is not _I32 or not t.is_cuda or device is not None and t.get_device() != device:
+        _refuse(f"block table: int32 tensor [sequences, pages]{_on(device)}")
     (n, m), (row, one) = t.shape, t.stride()
     if one != 1 and m > 1:
         _refuse("block table: rows that are contiguous")
@@ -469,12 +487,13 @@ def kv_layer(model, pool, layer):
 def vf_pages_assign(lens, new, free_pages, n_free, block_table, row_off, pos, slot, kv_len, n_free_out):
     """int32 device tensors: lens, new [n], free_pages [any], n_free [1], block_table [n, pages]; results row_off [n + 1],
     pos, slot [total rows], kv_len [n], n_free_out [1], and the fresh entries of block_table."""
-    n, m, stride = _table(block_table)
+    dev = _device("lens", lens)
+    n, m, stride = _table(block_table, dev)
     rows = pos.numel()
-    _check(lib.vf_pages_assign(n, m, stride, rows, free_pages.numel(), _ints("lens", lens, n), _ints("new", new, n),
-                               _ints("free_pages", free_pages, 0), _ints("n_free", n_free, 1), block_table.data_ptr(),
-                               _ints("row_off", row_off, n + 1), _ints("pos", pos, rows), _ints("slot", slot, rows),
-                               _ints("kv_len", kv_len, n), _ints("n_free_out", n_free_out, 1), _stream_of(lens)))
+    _check(lib.vf_pages_assign(n, m, stride, rows, free_pages.numel(), _ints("lens", lens, n, dev), _ints("new", new, n, dev),
+                               _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev), block_table.data_ptr(),
+                               _ints("row_off", row_off, n + 1, dev), _ints("pos", pos, rows, dev), _ints("slot", slot, rows, dev),
+                               _ints("kv_len", kv_len, n, dev), _ints("n_free_out", n_free_out, 1, dev), _stream_of(lens)))
 
 
 def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED, factor=1.0, low=0.0, high=0.0, trained=0.0,
@@ -490,30 +509,30 @@ def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HAL
     """q, q_out [rows, q heads, hd], k, v [rows, kv heads, hd] (views of wider rows allowed), table of vf_rotary_table, pos and
     slot int32 [rows], pool: one layer's pages (kv_layer)."""
     rows, hq, hd = q.shape
-    pages, hkv = _pool(pool, hd, q.dtype)
+    dt, dev = q.dtype, _device("q", q)
+    pages, hkv = _pool(pool, hd, dt, dev)
     positions, half, two = table.shape
-    if two != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or not table.is_cuda:
-        _refuse("table: contiguous float32 device tensor [positions, rotary_dim / 2, 2]")
-    dt = q.dtype
+    if two != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or not table.is_cuda or dev is not None and table.get_device() != dev:
+        _refuse(f"table: contiguous float32 tensor [positions, rotary_dim / 2, 2]{_on(dev)}")
     args = vf_rotary_args(_dtype(q), hq, hkv, hd, 2 * half, pairs, rows, positions, pages, 0,
-                          _rows("q", q, dt, rows, hq, hd), _rows("k", k, dt, rows, hkv, hd),
-                          _rows("v", v, dt, rows, hkv, hd), _rows("q_out", q_out, dt, rows, hq, hd))
+                          _rows("q", q, dt, rows, hq, hd, dev), _rows("k", k, dt, rows, hkv, hd, dev),
+                          _rows("v", v, dt, rows, hkv, hd, dev), _rows("q_out", q_out, dt, rows, hq, hd, dev))
     _check(lib.vf_rotary_append(C.byref(args), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                _ints("pos", pos, rows), _ints("slot", slot, rows), q_out.data_ptr(), pool.data_ptr(), _stream_of(q)))
+                                _ints("pos", pos, rows, dev), _ints("slot", slot, rows, dev), q_out.data_ptr(), pool.data_ptr(), _stream_of(q)))
 
 
-def _packed_args(q, pool, block_table, out, max_rows, max_keys, scale):
+def _packed_args(q, pool, block_table, out, max_rows, max_keys, scale, dev):
     rows, hq, hd = q.shape
-    pages, hkv = _pool(pool, hd, q.dtype)
-    n, m, stride = _table(block_table)
-    q_stride = _rows("q", q, q.dtype, rows, hq, hd)
+    pages, hkv = _pool(pool, hd, q.dtype, dev)
+    n, m, stride = _table(block_table, dev)
+    q_stride = _rows("q", q, q.dtype, rows, hq, hd, dev)
     return vf_packed_args(_dtype(q), hq, hkv, hd, n, rows, max_rows, max_keys, pages, m, stride, scale, q_stride,
-                          q_stride if out is None else _rows("out", out, q.dtype, rows, hq, hd))
+                          q_stride if out is None else _rows("out", out, q.dtype, rows, hq, hd, dev))
 
 
 def vf_attention_packed_workspace(q, pool, block_table, max_rows, max_keys):
     """A workspace for vf_attention_packed with these arguments: uint8 device tensor."""
-    n = lib.vf_attention_packed_workspace(C.byref(_packed_args(q, pool, block_table, None, max_rows, max_keys, 0.0)))
+    n = lib.vf_attention_packed_workspace(C.byref(_packed_args(q, pool, block_table, None, max_rows, max_keys, 0.0, _device("q", q))))
     if n == C.c_size_t(-1).value:
         raise VfError(VF_ERR_ARG, lib.vf_last_error().decode())
     return torch.empty(n, dtype=torch.uint8, device=q.device)
@@ -522,9 +541,10 @@ def vf_attention_packed_workspace(q, pool, block_table, max_rows, max_keys):
 def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, max_keys, workspace, scale=0.0):
     """q, out [rows, q heads, hd]; pool: one layer's pages; block_table int32 [n, pages]; row_off int32 [n + 1] and kv_len
     int32 [n] on the device; max_rows, max_keys: the host's bounds of a sequence's rows and keys."""
-    args = _packed_args(q, pool, block_table, out, max_rows, max_keys, scale)
-    if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
-        _refuse("workspace: contiguous uint8 device tensor")
+    dev = _device("q", q)
+    args = _packed_args(q, pool, block_table, out, max_rows, max_keys, scale, dev)
+    if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous() or dev is not None and workspace.get_device() != dev:
+        _refuse(f"workspace: contiguous uint8 tensor{_on(dev)}")
     _check(lib.vf_attention_packed(C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
-                                   _ints("row_off", row_off, args.n_seqs + 1), _ints("kv_len", kv_len, args.n_seqs),
+                                   _ints("row_off", row_off, args.n_seqs + 1, dev), _ints("kv_len", kv_len, args.n_seqs, dev),
                                    out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(q)))

@@ -844,7 +844,7 @@ struct TypeCost {
 constexpr TypeCost COST[3] = {
     {{{2.991f, 1.12f, 1.167f, 1.143f, 0.001f}, {6.042f, 0.6525f, 0.5752f, 0.4454f, 3.089f}, {1.302f, 0.2779f, 0.3042f, 0.09254f, 1.694f}, {4.439f, 0.4318f, 0.43f, 0.4294f, 0.2164f}}, 5.297f, 0.4362f, 1.178f},   // bfloat16, heads of 64
     {{{4.291f, 0.9058f, 0.7355f, 0.7817f, 1.317f}, {5.425f, 0.8706f, 0.5725f, 0.4849f, 2.104f}, {3.007f, 0.4337f, 0.3039f, 0.281f, 1.466f}, {4.181f, 0.6562f, 0.7576f, 0.5794f, 1.727f}}, 4.363f, 0.6175f, 2.549f},   // bfloat16, heads of 128
-    {{{2.321f, 5.142f, 7.635f, 1.674f, 0.5421f}, {}, {2.393f, 0.691f, 0.4236f, 0.622f, 0.001f}, {8.491f, 0.7689f, 1.807f, 1.221f, 1.31f}}, 4.161f, 1.255f, 0.001072f},   // float32
+    {{{2.321f, 5.142f, 7.635f, 1.674f, 0.5421f}, {/* no two groups */}, {2.393f, 0.691f, 0.4236f, 0.622f, 0.001f}, {8.491f, 0.7689f, 1.807f, 1.221f, 1.31f}}, 4.161f, 1.255f, 0.001072f},   // float32
 };
 
 Plan make_plan(const vf_packed_args &a) {
@@ -914,8 +914,14 @@ template <typename T, int HD, int KG> int launch_tiles(const PackedAttn &p, hipS
     VF_HIP(set);
     return start(attention_tiles_kernel<T, HD, KG>, (long long)p.tiles * p.parts * p.a.n_kv_heads, TILE_WAVES * KG * 64, LDS, p, st);
 }
+template <typename T, int HD> int launch_kernel(const PackedAttn &p, const Plan &plan, hipStream_t st) {
+    if (plan.kernel == FEW) return plan.waves == 4 ? launch_few<T, HD, 4>(p, st) : launch_few<T, HD, 8>(p, st);
+    if constexpr (sizeof(T) == 2)
+        if (plan.kernel == TILES_TWO) return launch_tiles<T, HD, 2>(p, st);
+    return launch_tiles<T, HD, 1>(p, st);
+}
 template <typename T, int HD> int launch(const PackedAttn &p, const Plan &plan, hipStream_t st) {
-    const int rc = plan.kernel == FEW ? (plan.waves == 4 ? launch_few<T, HD, 4>(p, st) : launch_few<T, HD, 8>(p, st)) : plan.kernel == TILES ? launch_tiles<T, HD, 1>(p, st) : launch_tiles<T, HD, sizeof(T) == 2 ? 2 : 1>(p, st);
+    const int rc = launch_kernel<T, HD>(p, plan, st);
     if (rc != VF_OK || p.parts == 1) return rc;
     constexpr int PER = 256 / (HD / 4);
     return start(attention_merge_kernel<T, HD>, ((long long)p.a.total_rows * p.a.n_q_heads + PER - 1) / PER, 256, 0, p, st);

@@ -426,7 +426,7 @@ size_t vf_attention_packed_workspace(const vf_packed_args *args);
  * p = kv_len[b] - rows_b + i and sees the keys 0 .. p of its pages:
  *   out[row][h] = sum_t softmax_t(scale * q[row][h] . K[t][h / group]) V[t][h / group]
  * Whole prompts (rows_b = kv_len[b]), chunks behind a cached prefix, drafts and single tokens may be mixed.
- * A row that sees no key (p < 0, or kv_len 0 for a refused sequence) gets zeros; a page id outside the pool
+ * A row that sees no key (p < 0, or kv_len 0 for a refused sequence; a negative kv_len counts as 0) gets zeros; a page id outside the pool
  * stands for 64 keys that are not there.  Keys that a row does not see add nothing to it, whatever memory
  * holds there (also where it is not finite).  Rows outside row_off[0] .. row_off[n_seqs] are not written.
  * bfloat16: scores, softmax and sums are float32, probabilities are rounded to bfloat16 for the product

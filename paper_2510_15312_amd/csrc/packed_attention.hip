@@ -160,9 +160,9 @@ template <int OFF> __device__ __forceinline__ int unit_to_lds(int order, const v
 //
 // What bounds it: a page of heads of 128 is 32 matrix instructions of 32 cycles among 135 on vectors and about 100 scalar and LDS
 // instructions of a wavefront, which issues one in four to five cycles; two wavefronts share a SIMD.  A prompt of 8192 tokens at 3B
-// (24 heads of 128, 8 of K and V) takes 373 to 394 us
-// = 1.05 to 1.1 PFLOP/s where a large matrix product reaches 1.3; the matrix units are busy 58 % of the cycles, at a clock that
-// the power limit has brought to 1.75 GHz.  20000 tokens at 1.5B: 1.12 PFLOP/s; at 0.5B (heads of 64, whose products are half as
+// (24 heads of 128, 8 of K and V) takes 373 to 396 us
+// = 1.04 to 1.1 PFLOP/s where a large matrix product reaches 1.3; the matrix units are busy 58 % of the cycles, at a clock that
+// the power limit has brought to 1.7 GHz.  20000 tokens at 1.5B: 1.12 PFLOP/s; at 0.5B (heads of 64, whose products are half as
 // long for the same softmax) 0.9.  Twelve prompts of 230 to 2048 tokens at 0.5B 59 us = 694 TFLOP/s: a tile has 16 pages on
 // average, of which the last one or two are masked, behind a start of three dependent reads.
 // Not taken, as no faster: three and four pages in flight, eight wavefronts on one page, a hand-laid order of the page's
@@ -316,6 +316,9 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
             for (int i = 0; i < 32; ++i) sc.t[i >> 4][i & 15] *= p.scale_log2e;
         }
     };
+    // Weights are rounded to bfloat16 for the product with V, which is bfloat16 itself: results are off by 2.0e-3 of their size where
+    // their own rounding is 1.6e-3.  A second bfloat16 value a weight, as the kernel for few items takes, would be half as many matrix
+    // instructions again, and 16 registers where heads of 128 have 5 left.
     auto weights = [&](const Scores &sc) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -525,7 +528,7 @@ __global__ __launch_bounds__(TILE_WAVES * KG * 64, (tile_waves_per_simd<T, HD, K
 // fragment of the pool is one contiguous kilobyte.  The wavefronts' sums meet in LDS.
 // Bound by bytes where there are enough sequences (32 tokens behind up to 8191 at 3B: 117 us = 5.0 TB/s, where a copy reaches 4.8; 64
 // behind up to 1999 at 1.5B 18.6 us = 3.8 TB/s), else by the launch and four dependent reads (lengths, page ids, keys, values): one token
-// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 8.4 us and 3 to 4 for the merge (2.6 TB/s in all).
+// behind 1023 at 0.5B 6.1 us, sixteen behind up to 4095 at 1.5B in parts 8.2 us and 3 to 4 for the merge (2.6 TB/s in all).
 // 16 items leave half of a 16x16 product empty for groups of 6 to 8 heads, which costs nothing here; 32 a workgroup were no faster.
 // Operands of a 16x16 product over 32 values of k: 16 lanes each take 8.
 __device__ __forceinline__ floatx4 mma16(const Frag<bf16_t> &a, const Frag<bf16_t> &b, floatx4 c) {

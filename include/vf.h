@@ -409,6 +409,21 @@ int vf_rotary_append(const vf_rotary_args *args, const void *q_dev, const void *
                      const float *table_dev, const int32_t *pos_dev, const int32_t *slot_dev, void *q_out_dev,
                      void *kv_layer_dev, void *stream);
 
+/* Norms of the queries and keys of every head: x * g / sqrt(mean of the head's x^2 + eps).  Gains are float32 [head_dim] for all heads
+ * of a side (stride 0) or one for every head, gain_stride elements apart; NULL: no gains.  eps > 0; gains at multiples of 16 bytes. */
+typedef struct {
+    const float *q_gain_dev, *k_gain_dev;
+    int32_t q_gain_stride, k_gain_stride;
+    float eps;
+    int32_t pad;
+} vf_head_norm;
+
+/* vf_rotary_append of queries and keys whose heads are normalised first; v as it is.  Squares and their sums are float32, as all
+ * else up to the one rounding at the end: a head's elements are at most about 1e18. */
+int vf_norm_rotary_append(const vf_rotary_args *args, const vf_head_norm *norm, const void *q_dev, const void *k_dev,
+                          const void *v_dev, const float *table_dev, const int32_t *pos_dev, const int32_t *slot_dev,
+                          void *q_out_dev, void *kv_layer_dev, void *stream);
+
 typedef struct {
     int32_t dtype, n_q_heads, n_kv_heads, head_dim;
     int32_t n_seqs, total_rows;
@@ -435,6 +450,96 @@ int vf_attention_packed(const vf_packed_args *args, const void *q_dev, const voi
                         const int32_t *block_table_dev, const int32_t *row_off_dev,
                         const int32_t *kv_len_dev, void *out_dev, void *workspace_dev,
                         size_t workspace_bytes, void *stream);
+
+/* ---- requests that branch, are cut back or move (next to packed batches) ----------------------- */
+
+/* Sequences may share full pages: shares[page] is the number of block tables that hold a page beyond the first, 0 for a page that one
+ * sequence holds and for a free one (vf_pages_assign leaves it so).  A page that is not full is never shared, so that what is written behind a
+ * sequence's tokens is its own; the calls below keep that.  All arrays are int32 on the device: block_table [n_seqs][max_pages] with
+ * rows table_stride apart, len [n_seqs], shares [pool_pages], free_pages [free_entries] with n_free [1] entries, the end taken first.  A length
+ * below 0 counts as 0, one above 64 * max_pages as that; page ids outside the pool are passed on and never counted, freed or copied.
+ * n_seqs * max_pages is at most 2^30.  Results do not depend on timing. */
+#define VF_PAGES_MAX_POOL (1 << 18)   /* pages of a pool of these calls */
+typedef struct {
+    int32_t n_seqs, max_pages, table_stride, pool_pages, free_entries, pad;
+} vf_pages_args;
+
+/* Fork i makes the empty sequence dst[i] a copy of the first tokens[i] tokens of sequence src[i] (all of them if tokens[i] is negative
+ * or more than it holds).  Full pages are shared; of a last page that is not full the fork gets a copy, in a page off the free list:
+ * copies[k] = {page, its copy} for the k-th such fork, n_copies[0] of them, to be done by vf_pages_copy on every layer.
+ * Nothing happens for a fork whose src or dst is no sequence, whose dst holds tokens, or whose dst an earlier fork of the call names; one that
+ * needs a page is refused, and its dst stays empty, if it and the forks before it need more than n_free together.
+ *   kv_len[n_seqs]   len with the forks' lengths entered;  n_free_out[1]   entries left in the free list
+ * and the granted forks' entries of block_table and counts of shares.  A src that is a dst of the same call is taken as it was: empty. */
+int vf_pages_fork(const vf_pages_args *args, int n_forks, const int32_t *src_dev, const int32_t *dst_dev, const int32_t *tokens_dev,
+                  const int32_t *len_dev, const int32_t *free_pages_dev, const int32_t *n_free_dev, int32_t *block_table_dev,
+                  int32_t *shares_dev, int32_t *kv_len_dev, int32_t *n_free_out_dev, int32_t *copies_dev, int32_t *n_copies_dev,
+                  void *stream);
+
+/* Of sequence b the first keep[b] tokens stay (all, if keep[b] is negative or not below len[b]).  The pages behind them are dropped from its table
+ * (their entries become -1); one that no sequence holds any more goes on the end of free_pages, in the order in which the dropped entries first
+ * name them, sequence by sequence.  Where a sequence is cut inside a page that others hold too, it gets a copy of that page, off the free list as it is by
+ * then, in the order of the sequences (copies [n_seqs][2] and n_copies as in vf_pages_fork); if all holders of a page are cut inside
+ * it, the last of them keeps it.  A sequence for whose copy no page is left keeps its full pages only.
+ *   kv_len[n_seqs]   tokens that it holds now;  n_free_out[1]   entries of the free list; entries past free_entries are lost
+ * and block_table, shares and free_pages, which change in place. */
+int vf_pages_keep(const vf_pages_args *args, const int32_t *len_dev, const int32_t *keep_dev, int32_t *free_pages_dev,
+                  const int32_t *n_free_dev, int32_t *block_table_dev, int32_t *shares_dev, int32_t *kv_len_dev,
+                  int32_t *n_free_out_dev, int32_t *copies_dev, int32_t *n_copies_dev, void *stream);
+
+/* The pages that sequences hold get the numbers 0, 1, .. in the order of their old ones, for a pool of `room` pages: the batch can go
+ * on in a smaller or larger pool, or be kept as it is now.  args->free_entries is not read.
+ *   table_out [n_seqs][max_pages]  the tables with the new numbers, rows table_out_stride apart, -1 behind a sequence's pages (block_table itself allowed, with its stride)
+ *   moved [pool_pages]             a page's new number, -1: nobody holds it
+ *   shares_out [room], free_out [room], n_free_out [1]   share counts, and the free list room - 1 .. (its first entry the page behind the held ones)
+ *   copies [min(pool_pages, room)][2], n_copies [1]      for vf_pages_copy, from the one pool to the other
+ * If more than `room` pages are held, those from number `room` on are lost (-1 in table_out and moved). */
+int vf_pages_compact(const vf_pages_args *args, int room, int table_out_stride, const int32_t *len_dev, const int32_t *block_table_dev,
+                     const int32_t *shares_dev, int32_t *table_out_dev, int32_t *shares_out_dev, int32_t *free_out_dev,
+                     int32_t *n_free_out_dev, int32_t *moved_dev, int32_t *copies_dev, int32_t *n_copies_dev, void *stream);
+
+/* Layers of pages of page_bytes each (2 * n_kv_heads * 64 * head_dim elements), layer strides in bytes; max_copies = room of copies. */
+typedef struct {
+    int32_t n_layers, page_bytes, src_pages, dst_pages, max_copies, pad;
+    int64_t src_layer_stride, dst_layer_stride;
+} vf_copy_args;
+
+/* Page copies[k][0] of every layer of src goes to page copies[k][1] of dst, k < n_copies[0] (at most max_copies); src and dst may be one
+ * pool.  A pair with a page outside its pool is left out.  No page is named as a target twice, or as a target and (in one pool) a source. */
+int vf_pages_copy(const vf_copy_args *args, const void *src_dev, void *dst_dev, const int32_t *copies_dev,
+                  const int32_t *n_copies_dev, void *stream);
+
+/* ---- penalties, biases and masks on logits (between vf_verify and vf_accept, or in a packed batch) ---------- */
+
+#define VF_LOGITS_MAX_VOCAB   (1 << 24)
+#define VF_LOGITS_MAX_HISTORY (1 << 24)
+typedef struct {
+    int32_t dtype;                  /* of the logits read (VF_F32 | VF_BF16); results are float32 */
+    int32_t n_seqs, total_rows, vocab;
+    int32_t max_history;            /* entries of a history that may be read                      */
+    int32_t bias_entries, mask_rows, pad;
+    int64_t in_stride, out_stride;  /* elements between rows                                      */
+    int64_t history_stride;         /* entries between histories                                  */
+    int64_t mask_stride;            /* words between masks                                        */
+} vf_logits_args;
+
+/* Logits z of the rows row_off[b] .. row_off[b + 1] - 1 of sequence b, one after the other:
+ *   z = z > 0 ? z / rho : z * rho        for ids that the row's text has                 rho, alpha, beta = penalties[b]
+ *   z = z - (alpha + beta * n)           for ids that its text has n > 0 times behind the prompt
+ *   z = z + bias                         for the ids bias_id[bias_off[b] .. bias_off[b + 1] - 1]
+ *   z = -infinity                        where the row's mask has a 0
+ * The text of row r is history[b][0 .. history_len[b]), whose first prompt_len[b] tokens are the prompt, and, behind it, the tokens of the
+ * sequence's rows up to and with r (tokens[total_rows]: the pending token and the drafts of a verify step, which the history
+ * must not have yet).  Ids outside the vocabulary (VF_PENDING too) count nowhere; of several biases of an id the last counts.  Row r has mask
+ * mask_row[r] (a number outside 0 .. mask_rows - 1: none), id v is bit v % 32 of its word v / 32.  A row whose mask leaves nothing is all
+ * -infinity.  penalties is float32 [n_seqs][3], rho > 0.  NULL stands for no penalties, no history, no prompt, no row tokens, no
+ * biases, no masks; with mask_row NULL row r has mask r.  Arithmetic is float32.  out may be logits (float32, the same stride).  Rows outside the
+ * sequences are not written. */
+int vf_logits_adjust(const vf_logits_args *args, const void *logits_dev, const int32_t *row_off_dev, float *out_dev,
+                     const float *penalties_dev, const int32_t *history_dev, const int32_t *history_len_dev,
+                     const int32_t *prompt_len_dev, const int32_t *tokens_dev, const int32_t *bias_off_dev,
+                     const int32_t *bias_id_dev, const float *bias_dev, const uint32_t *mask_dev,
+                     const int32_t *mask_row_dev, void *stream);
 
 /* ---- options ---------------------------------------------------------------------------------- */
 

@@ -25,6 +25,8 @@ VF_OPT_FAST_PATH = 1
 VF_OPT_PERSISTENT = 2
 VF_PACKED_MAX_SEQS, VF_PACKED_MAX_ROWS = 4096, 1 << 20
 VF_ROTARY_HALF, VF_ROTARY_INTERLEAVED = 0, 1
+VF_PAGES_MAX_POOL = 1 << 18
+VF_LOGITS_MAX_VOCAB, VF_LOGITS_MAX_HISTORY = 1 << 24, 1 << 24
 VF_ROTARY_UNSCALED, VF_ROTARY_POSITIONS, VF_ROTARY_BASE, VF_ROTARY_RAMP = 0, 1, 2, 3
 
 EXPORTS = [
@@ -35,6 +37,7 @@ EXPORTS = [
     "vf_reuse_select", "vf_reuse_pool_init", "vf_reuse_pool_update", "vf_reuse_pool_extend",
     "vf_verify_tree", "vf_accept_tree", "vf_prefill_chunk_topk", "vf_draft_suffix_match",
     "vf_pages_assign", "vf_rotary_table", "vf_rotary_append", "vf_attention_packed_workspace", "vf_attention_packed",
+    "vf_norm_rotary_append", "vf_pages_fork", "vf_pages_keep", "vf_pages_compact", "vf_pages_copy", "vf_logits_adjust",
 ]
 SITES = ["qkv", "o", "gateup", "down", "head", "attn", "small", "accept", "step"]
 
@@ -81,6 +84,25 @@ class vf_rotary_args(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "pairs",
                                          "total_rows", "max_positions", "pool_pages", "pad")] + \
                [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
+
+
+class vf_head_norm(C.Structure):
+    _fields_ = [("q_gain_dev", C.c_void_p), ("k_gain_dev", C.c_void_p), ("q_gain_stride", C.c_int32), ("k_gain_stride", C.c_int32),
+                ("eps", C.c_float), ("pad", C.c_int32)]
+
+
+class vf_pages_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "max_pages", "table_stride", "pool_pages", "free_entries", "pad")]
+
+
+class vf_copy_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "page_bytes", "src_pages", "dst_pages", "max_copies", "pad")] + \
+               [(n, C.c_int64) for n in ("src_layer_stride", "dst_layer_stride")]
+
+
+class vf_logits_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_seqs", "total_rows", "vocab", "max_history", "bias_entries", "mask_rows", "pad")] + \
+               [(n, C.c_int64) for n in ("in_stride", "out_stride", "history_stride", "mask_stride")]
 
 
 class vf_packed_args(C.Structure):
@@ -133,6 +155,12 @@ def _load():
         "vf_rotary_append": (C.c_int, [C.POINTER(vf_rotary_args)] + [vp] * 9),
         "vf_attention_packed_workspace": (sz, [C.POINTER(vf_packed_args)]),
         "vf_attention_packed": (C.c_int, [C.POINTER(vf_packed_args)] + [vp] * 7 + [sz, vp]),
+        "vf_norm_rotary_append": (C.c_int, [C.POINTER(vf_rotary_args), C.POINTER(vf_head_norm)] + [vp] * 9),
+        "vf_pages_fork": (C.c_int, [C.POINTER(vf_pages_args), C.c_int] + [vp] * 13),
+        "vf_pages_keep": (C.c_int, [C.POINTER(vf_pages_args)] + [vp] * 11),
+        "vf_pages_compact": (C.c_int, [C.POINTER(vf_pages_args), C.c_int, C.c_int] + [vp] * 11),
+        "vf_pages_copy": (C.c_int, [C.POINTER(vf_copy_args)] + [vp] * 5),
+        "vf_logits_adjust": (C.c_int, [C.POINTER(vf_logits_args)] + [vp] * 14),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -505,20 +533,48 @@ def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED
     return table
 
 
-def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HALF):
-    """q, q_out [rows, q heads, hd], k, v [rows, kv heads, hd] (views of wider rows allowed), table of vf_rotary_table, pos and
-    slot int32 [rows], pool: one layer's pages (kv_layer)."""
+def _rotary_args(q, k, v, table, q_out, pool, pairs, dev):
     rows, hq, hd = q.shape
-    dt, dev = q.dtype, _device("q", q)
+    dt = q.dtype
     pages, hkv = _pool(pool, hd, dt, dev)
     positions, half, two = table.shape
     if two != 2 or table.dtype is not torch.float32 or not table.is_contiguous() or not table.is_cuda or dev is not None and table.get_device() != dev:
         _refuse(f"table: contiguous float32 tensor [positions, rotary_dim / 2, 2]{_on(dev)}")
-    args = vf_rotary_args(_dtype(q), hq, hkv, hd, 2 * half, pairs, rows, positions, pages, 0,
+    return vf_rotary_args(_dtype(q), hq, hkv, hd, 2 * half, pairs, rows, positions, pages, 0,
                           _rows("q", q, dt, rows, hq, hd, dev), _rows("k", k, dt, rows, hkv, hd, dev),
                           _rows("v", v, dt, rows, hkv, hd, dev), _rows("q_out", q_out, dt, rows, hq, hd, dev))
+
+
+def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HALF):
+    """q, q_out [rows, q heads, hd], k, v [rows, kv heads, hd] (views of wider rows allowed), table of vf_rotary_table, pos and
+    slot int32 [rows], pool: one layer's pages (kv_layer)."""
+    dev = _device("q", q)
+    args = _rotary_args(q, k, v, table, q_out, pool, pairs, dev)
     _check(lib.vf_rotary_append(C.byref(args), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                _ints("pos", pos, rows, dev), _ints("slot", slot, rows, dev), q_out.data_ptr(), pool.data_ptr(), _stream_of(q)))
+                                _ints("pos", pos, args.total_rows, dev), _ints("slot", slot, args.total_rows, dev), q_out.data_ptr(),
+                                pool.data_ptr(), _stream_of(q)))
+
+
+def _gain(name, t, heads, hd, dev):
+    """(address, stride between heads) of gains [hd] or [heads, hd]; None: no gains."""
+    if t is None:
+        return None, 0
+    if t.dtype is not torch.float32 or not t.is_cuda or not t.is_contiguous() or dev is not None and t.get_device() != dev or \
+            tuple(t.shape) not in ((hd,), (heads, hd)):
+        _refuse(f"{name}: contiguous float32 tensor [{hd}] or [{heads}, {hd}]{_on(dev)}")
+    return t.data_ptr(), hd if t.dim() == 2 else 0
+
+
+def vf_norm_rotary_append(q, k, v, q_gain, k_gain, eps, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HALF):
+    """As vf_rotary_append, with every head of q and k normalised first: x * gain / sqrt(mean x^2 + eps).  q_gain, k_gain: float32
+    [hd] or [heads, hd], or None."""
+    dev = _device("q", q)
+    args = _rotary_args(q, k, v, table, q_out, pool, pairs, dev)
+    (qg, qs), (kg, ks) = _gain("q_gain", q_gain, args.n_q_heads, args.head_dim, dev), _gain("k_gain", k_gain, args.n_kv_heads, args.head_dim, dev)
+    norm = vf_head_norm(qg, kg, qs, ks, eps, 0)
+    _check(lib.vf_norm_rotary_append(C.byref(args), C.byref(norm), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                                     _ints("pos", pos, args.total_rows, dev), _ints("slot", slot, args.total_rows, dev),
+                                     q_out.data_ptr(), pool.data_ptr(), _stream_of(q)))
 
 
 def _packed_args(q, pool, block_table, out, max_rows, max_keys, scale, dev):
@@ -548,3 +604,118 @@ def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, ma
     _check(lib.vf_attention_packed(C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
                                    _ints("row_off", row_off, args.n_seqs + 1, dev), _ints("kv_len", kv_len, args.n_seqs, dev),
                                    out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(q)))
+
+
+# ---- requests that branch, are cut back or move --------------------------------------------------
+
+def _pages_args(block_table, shares, free_entries, dev):
+    n, m, stride = _table(block_table, dev)
+    return vf_pages_args(n, m, stride, shares.numel(), free_entries, 0)
+
+
+def vf_pages_fork(src, dst, tokens, lens, free_pages, n_free, block_table, shares, kv_len, n_free_out, copies, n_copies):
+    """int32 device tensors: src, dst, tokens [forks], lens [n], free_pages [any], n_free [1], block_table [n, pages], shares [pool
+    pages]; results kv_len [n], n_free_out [1], copies [forks, 2], n_copies [1], and what changes in block_table and shares."""
+    dev = _device("lens", lens)
+    a, forks = _pages_args(block_table, shares, free_pages.numel(), dev), src.numel()
+    _check(lib.vf_pages_fork(C.byref(a), forks, _ints("src", src, forks, dev), _ints("dst", dst, forks, dev), _ints("tokens", tokens, forks, dev),
+                             _ints("lens", lens, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev),
+                             block_table.data_ptr(), _ints("shares", shares, 1, dev), _ints("kv_len", kv_len, a.n_seqs, dev),
+                             _ints("n_free_out", n_free_out, 1, dev), _ints("copies", copies, 2 * forks, dev), _ints("n_copies", n_copies, 1, dev),
+                             _stream_of(lens)))
+
+
+def vf_pages_keep(lens, keep, free_pages, n_free, block_table, shares, kv_len, n_free_out, copies, n_copies):
+    """int32 device tensors: lens, keep [n], n_free [1], and free_pages [any], block_table [n, pages], shares [pool pages], which change
+    in place; results kv_len [n], n_free_out [1], copies [n, 2], n_copies [1]."""
+    dev = _device("lens", lens)
+    a = _pages_args(block_table, shares, free_pages.numel(), dev)
+    _check(lib.vf_pages_keep(C.byref(a), _ints("lens", lens, a.n_seqs, dev), _ints("keep", keep, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev),
+                             _ints("n_free", n_free, 1, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
+                             _ints("kv_len", kv_len, a.n_seqs, dev), _ints("n_free_out", n_free_out, 1, dev),
+                             _ints("copies", copies, 2 * a.n_seqs, dev), _ints("n_copies", n_copies, 1, dev), _stream_of(lens)))
+
+
+def vf_pages_compact(lens, block_table, shares, table_out, shares_out, free_out, n_free_out, moved, copies, n_copies):
+    """int32 device tensors: lens [n], block_table [n, pages], shares [pool pages]; results table_out [n, pages] (block_table itself
+    allowed), shares_out and free_out [pages of the new pool], n_free_out [1], moved [pool pages], copies [pool pages, 2], n_copies [1]."""
+    dev = _device("lens", lens)
+    a, room = _pages_args(block_table, shares, 0, dev), shares_out.numel()
+    n, m, stride = _table(table_out, dev)
+    if (n, m) != (a.n_seqs, a.max_pages):
+        _refuse(f"table_out: int32 tensor [{a.n_seqs}, {a.max_pages}]{_on(dev)}")
+    _check(lib.vf_pages_compact(C.byref(a), room, stride, _ints("lens", lens, a.n_seqs, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
+                                table_out.data_ptr(), _ints("shares_out", shares_out, 1, dev), _ints("free_out", free_out, room, dev),
+                                _ints("n_free_out", n_free_out, 1, dev), _ints("moved", moved, a.pool_pages, dev),
+                                _ints("copies", copies, 2 * min(a.pool_pages, room), dev), _ints("n_copies", n_copies, 1, dev), _stream_of(lens)))
+
+
+def _layers(name, t, dev):
+    """(layers, pages, bytes a page, bytes between layers) of pages [layers, pages, ...] or of one layer's, [pages, 2, kv heads, 64 * hd]."""
+    if t.dim() == 4:
+        t = t[None]
+    if t.dim() != 5 or not t.is_cuda or not t[0].is_contiguous() or dev is not None and t.get_device() != dev:
+        _refuse(f"{name}: tensor [layers, pages, 2, kv heads, 64 * head_dim] whose layers are contiguous{_on(dev)}")
+    return t.shape[0], t.shape[1], t[0, 0].numel() * t.element_size(), t.stride(0) * t.element_size()
+
+
+def vf_pages_copy(pools, copies, n_copies, to):
+    """pools, to: [layers, pages, 2, kv heads, 64 * hd] of all layers (or one layer without that dimension), of one type, which may be the same;
+    copies int32 [any, 2], n_copies int32 [1] on the device."""
+    dev = _device("pools", pools)
+    layers, pages, size, stride = _layers("pools", pools, dev)
+    to_layers, to_pages, to_size, to_stride = _layers("to", to, dev)
+    if (to_layers, to_size) != (layers, size) or to.dtype is not pools.dtype:
+        _refuse("pools of other layers, heads or types")
+    a = vf_copy_args(layers, size, pages, to_pages, copies.numel() // 2, 0, stride, to_stride)
+    _check(lib.vf_pages_copy(C.byref(a), pools.data_ptr(), to.data_ptr(), _ints("copies", copies, 0, dev), _ints("n_copies", n_copies, 1, dev),
+                             _stream_of(pools)))
+
+
+# ---- logits ----------------------------------------------------------------------------------------
+
+def _matrix(name, t, dtype, rows, columns, dev):
+    """The row stride of a device tensor [rows, columns] whose rows are contiguous; None for any number stands for any."""
+    if t.dim() != 2 or t.dtype is not dtype or not t.is_cuda or dev is not None and t.get_device() != dev or \
+            rows is not None and t.shape[0] != rows or columns is not None and t.shape[1] != columns:
+        _refuse(f"{name}: tensor [{'any' if rows is None else rows}, {'any' if columns is None else columns}] of {dtype}{_on(dev)}")
+    row, one = t.stride()
+    if one != 1 and t.shape[1] > 1:
+        _refuse(f"{name}: rows that are contiguous")
+    return row if t.shape[0] > 1 else max(row, t.shape[1])
+
+
+def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history_len=None, prompt_len=None, tokens=None, biases=None,
+                     mask=None, mask_row=None):
+    """logits [rows, vocab] in bfloat16 or float32, out [rows, vocab] in float32 (logits itself allowed), row_off int32 [n + 1];
+    penalties float32 [n, 3] (repetition, presence, frequency), history int32 [n, any], history_len and prompt_len int32 [n], tokens
+    int32 [rows], biases: int32 offsets [n + 1], int32 ids and float32 values [any]; mask int32 [any, at least vocab / 32] (a bit an id),
+    mask_row int32 [rows].  What is None is left out."""
+    dev = _device("logits", logits)
+    if logits.dim() != 2:
+        _refuse(f"logits: tensor [rows, vocab]{_on(dev)}")
+    (rows, vocab), n = logits.shape, row_off.numel() - 1
+    in_stride, out_stride = _matrix("logits", logits, logits.dtype, rows, vocab, dev), _matrix("out", out, torch.float32, rows, vocab, dev)
+
+    def ints(name, t, k):
+        return None if t is None else _ints(name, t, k, dev)
+    a = vf_logits_args(_dtype(logits), n, rows, vocab, 0, 0, 0, 0, in_stride, out_stride, 0, 0)
+    if penalties is not None and (_matrix("penalties", penalties, torch.float32, n, 3, dev) != 3):
+        _refuse(f"penalties: contiguous float32 tensor [{n}, 3]{_on(dev)}")
+    if history is not None:
+        a.history_stride, a.max_history = _matrix("history", history, _I32, n, None, dev), history.shape[1]
+    if mask is not None:
+        a.mask_stride, a.mask_rows = _matrix("mask", mask, _I32, None, None, dev), mask.shape[0]
+        if 32 * mask.shape[1] < vocab or mask_row is None and mask.shape[0] < rows:
+            _refuse(f"mask: a bit for each of {vocab} ids, and a row for each row without mask_row")
+    bias_off, bias_id, bias = biases if biases is not None else (None, None, None)
+    if bias_off is not None:
+        a.bias_entries = bias_id.numel()
+        if bias.dtype is not torch.float32 or not bias.is_cuda or not bias.is_contiguous() or bias.numel() != a.bias_entries or \
+                dev is not None and bias.get_device() != dev:
+            _refuse(f"biases: contiguous float32 tensor of {a.bias_entries} entries{_on(dev)}")
+    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _check(lib.vf_logits_adjust(C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), address(penalties), address(history),
+                                ints("history_len", history_len, n), ints("prompt_len", prompt_len, n), ints("tokens", tokens, rows),
+                                ints("bias_off", bias_off, n + 1), ints("bias_id", bias_id, 0), address(bias), address(mask),
+                                ints("mask_row", mask_row, rows), _stream_of(logits)))

@@ -2,6 +2,7 @@
 // the cache.  (Attention: packed_attention.hip.)
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "lds_stream.h"
 #include "vf_internal.h"
@@ -157,19 +158,16 @@ __device__ __forceinline__ Unit unit_of(int u, int rotary_dim, bool half) {
     if (half && turns) return {u * 8, rotary_dim / 2 + u * 8, true};
     return {u * 16, u * 16 + 8, turns};
 }
-template <typename T> __device__ __forceinline__ void turn_unit(Eight<T> &lo, Eight<T> &hi, const float2 *angle, bool half) {
-    float x[16], y[16];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { x[i] = to_f32(lo.v[i]); x[8 + i] = to_f32(hi.v[i]); }
+// x: eight elements of the unit's lower piece, eight of its upper one
+__device__ __forceinline__ void turn_unit(float *x, const float2 *angle, bool half) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float2 a = angle[i];
         const int p = half ? i : 2 * i, q = half ? 8 + i : 2 * i + 1;
-        y[p] = x[p] * a.x - x[q] * a.y;
-        y[q] = x[q] * a.x + x[p] * a.y;
+        const float lo = x[p] * a.x - x[q] * a.y, hi = x[q] * a.x + x[p] * a.y;
+        x[p] = lo;
+        x[q] = hi;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { lo.v[i] = from_f32<T>(y[i]); hi.v[i] = from_f32<T>(y[8 + i]); }
 }
 
 // What bounds it is memory, and how the cache is written.  A page keeps four consecutive tokens' eight-element pieces of K next
@@ -184,10 +182,14 @@ constexpr int ROTARY_ROWS = 16, ROTARY_V_ROWS = 64, BATCH = 4;
 
 struct RotaryGrid { int32_t heads, v, k, v_rows, v_single; };   // heads a workgroup of q or k; workgroups of v, of k; rows a workgroup of v; each by itself
 
-template <typename T, int HD, bool HALF>
-__device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const T *src, int64_t src_stride, const float2 *table, const int32_t *pos,
-                                            const int32_t *slot, T *out, bool is_k, int row, int ui, int h, int h1) {
+struct HeadNorms { vf_head_norm n; };                      // norms of q and k before they turn
+struct NoNorms {};
+
+template <typename T, int HD, bool HALF, typename NORM>
+__device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const NORM &norm, const T *src, int64_t src_stride, const float2 *table,
+                                            const int32_t *pos, const int32_t *slot, T *out, bool is_k, int row, int ui, int h, int h1) {
     constexpr int SIDE = 256 / (ROTARY_ROWS * (HD / 16));   // heads side by side
+    constexpr bool NORMED = std::is_same<NORM, HeadNorms>::value;
     if (row >= a.total_rows) return;
     const Unit u = unit_of(ui, a.rotary_dim, HALF);
     const int p = pos[row], s = is_k ? slot[row] : 0;
@@ -201,6 +203,17 @@ __device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const T *sr
             const float4 x = from[i];
             angle[2 * i] = make_float2(x.x, x.y);
             angle[2 * i + 1] = make_float2(x.z, x.w);
+        }
+    }
+    const float *gains = nullptr;
+    int gain_stride = 0;
+    Eight<float> gain_lo, gain_hi;
+    if constexpr (NORMED) {
+        gains = is_k ? norm.n.k_gain_dev : norm.n.q_gain_dev;
+        gain_stride = is_k ? norm.n.k_gain_stride : norm.n.q_gain_stride;
+        if (gains) {
+            gain_lo = eight(gains + u.lo);
+            gain_hi = eight(gains + u.hi);
         }
     }
     src += row * src_stride;
@@ -226,7 +239,36 @@ __device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const T *sr
         for (int i = 0; i < BATCH; ++i) {
             const int head = h + i * SIDE;
             if (head >= h1) break;
-            if (u.turns) turn_unit(lo[i], hi[i], angle, HALF);
+            if (NORMED || u.turns) {
+                float x[16];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { x[j] = to_f32(lo[i].v[j]); x[8 + j] = to_f32(hi[i].v[j]); }
+                if constexpr (NORMED) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum += x[j] * x[j];
+                    // the head's other units are the neighbouring lanes (q), or eight or sixteen lanes apart (k)
+#pragma unroll
+                    for (int d = 1; d < HD / 16; d <<= 1) sum += __shfl_xor(sum, is_k ? d * (64 / (HD / 16)) : d, 64);
+                    const float scale = 1.0f / sqrtf(sum * (1.0f / HD) + norm.n.eps);
+                    if (gain_stride) {
+                        gain_lo = eight(gains + (size_t)head * gain_stride + u.lo);
+                        gain_hi = eight(gains + (size_t)head * gain_stride + u.hi);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] *= scale;
+                        x[8 + j] *= scale;
+                        if (gains) {
+                            x[j] *= gain_lo.v[j];
+                            x[8 + j] *= gain_hi.v[j];
+                        }
+                    }
+                }
+                if (u.turns) turn_unit(x, angle, HALF);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { lo[i].v[j] = from_f32<T>(x[j]); hi[i].v[j] = from_f32<T>(x[8 + j]); }
+            }
             if (!at) lo[i] = hi[i] = Eight<T>{};
             put_eight(out + to_lo + (size_t)head * per_head, lo[i]);
             put_eight(out + to_hi + (size_t)head * per_head, hi[i]);
@@ -234,8 +276,8 @@ __device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const T *sr
     }
 }
 
-template <typename T, int HD, bool HALF>
-__global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, RotaryGrid g, const T *q, const T *__restrict__ k,
+template <typename T, int HD, bool HALF, typename NORM>
+__global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, NORM norm, RotaryGrid g, const T *q, const T *__restrict__ k,
                                                             const T *__restrict__ v, const float2 *__restrict__ table,
                                                             const int32_t *__restrict__ pos, const int32_t *__restrict__ slot,
                                                             T *q_out, T *__restrict__ kv) {
@@ -245,14 +287,17 @@ __global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, Ro
     if (w >= g.k + g.v) {
         w -= g.k + g.v;
         const int per = (hq + g.heads - 1) / g.heads, h0 = w % per * g.heads;
-        rotate_rows<T, HD, HALF>(a, q, a.q_stride, table, pos, slot, q_out, false, w / per * ROTARY_ROWS + tid / (UNITS * SIDE), tid % UNITS,
+        rotate_rows<T, HD, HALF>(a, norm, q, a.q_stride, table, pos, slot, q_out, false, w / per * ROTARY_ROWS + tid / (UNITS * SIDE), tid % UNITS,
                                  h0 + tid / UNITS % SIDE, min(h0 + g.heads, hq));
         return;
     }
     if (w >= g.v) {
         w = die_order(w - g.v, g.k);
         const int per = (hkv + g.heads - 1) / g.heads, h0 = w % per * g.heads;
-        rotate_rows<T, HD, HALF>(a, k, a.k_stride, table, pos, slot, kv, true, w / per * ROTARY_ROWS + tid % ROTARY_ROWS, tid / ROTARY_ROWS % UNITS,
+        // a head's units in one wavefront where they are summed over
+        const int across = std::is_same<NORM, HeadNorms>::value ? 64 / UNITS : ROTARY_ROWS;
+        const int row = tid % across + tid / (across * UNITS) % (ROTARY_ROWS / across) * across;
+        rotate_rows<T, HD, HALF>(a, norm, k, a.k_stride, table, pos, slot, kv, true, w / per * ROTARY_ROWS + row, tid / across % UNITS,
                                  h0 + tid / (ROTARY_ROWS * UNITS), min(h0 + g.heads, hkv));
         return;
     }
@@ -315,8 +360,8 @@ __global__ __launch_bounds__(256) void rotary_append_kernel(vf_rotary_args a, Ro
     }
 }
 
-template <typename T, int HD>
-int launch_rotary(const vf_rotary_args &a, const void *q, const void *k, const void *v, const float *table, const int32_t *pos,
+template <typename T, int HD, typename NORM>
+int launch_rotary(const char *name, const vf_rotary_args &a, const NORM &norm, const void *q, const void *k, const void *v, const float *table, const int32_t *pos,
                   const int32_t *slot, void *q_out, void *kv, hipStream_t st) {
     const int tiles = (a.total_rows + ROTARY_ROWS - 1) / ROTARY_ROWS, side = 256 / (ROTARY_ROWS * (HD / 16));
     RotaryGrid g;
@@ -330,14 +375,56 @@ int launch_rotary(const vf_rotary_args &a, const void *q, const void *k, const v
     const long long n_q = (long long)tiles * ((a.n_q_heads + g.heads - 1) / g.heads), n_k = (long long)tiles * ((a.n_kv_heads + g.heads - 1) / g.heads);
     const long long n_v = (long long)((a.total_rows + g.v_rows - 1) / g.v_rows) * a.n_kv_heads, blocks = n_q + n_k + n_v;
     if (blocks > 0xffffff)
-        return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: %d rows of %d heads in one call", a.total_rows, a.n_q_heads + 2 * a.n_kv_heads);
+        return vf_fail(VF_ERR_UNSUPPORTED, "%s: %d rows of %d heads in one call", name, a.total_rows, a.n_q_heads + 2 * a.n_kv_heads);
     g.v = (int32_t)n_v;
     g.k = (int32_t)n_k;
-    const auto kernel = a.pairs == VF_ROTARY_HALF ? rotary_append_kernel<T, HD, true> : rotary_append_kernel<T, HD, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, g, (const T *)q, (const T *)k, (const T *)v, (const float2 *)table,
+    const auto kernel = a.pairs == VF_ROTARY_HALF ? rotary_append_kernel<T, HD, true, NORM> : rotary_append_kernel<T, HD, false, NORM>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, norm, g, (const T *)q, (const T *)k, (const T *)v, (const float2 *)table,
                        pos, slot, (T *)q_out, (T *)kv);
     VF_LAUNCH_CHECK("rotary_append");
     return VF_OK;
+}
+
+// Both entry points: without norms, and with.
+template <typename NORM>
+int rotary_append(const char *name, const vf_rotary_args *args, const NORM &norm, const void *q_dev, const void *k_dev, const void *v_dev,
+                  const float *table_dev, const int32_t *pos_dev, const int32_t *slot_dev, void *q_out_dev, void *kv_layer_dev, void *stream) {
+    if (!args) return vf_fail(VF_ERR_ARG, "%s: NULL argument", name);
+    const vf_rotary_args &a = *args;
+    if (a.dtype != VF_F32 && a.dtype != VF_BF16) return vf_fail(VF_ERR_ARG, "%s: dtype %d", name, a.dtype);
+    if (a.n_q_heads < 1 || a.n_kv_heads < 1 || a.n_q_heads > 256 || a.n_kv_heads > 256)
+        return vf_fail(VF_ERR_ARG, "%s: %d query heads, %d key heads", name, a.n_q_heads, a.n_kv_heads);
+    if (a.head_dim != 64 && a.head_dim != 128) return vf_fail(VF_ERR_UNSUPPORTED, "%s: head_dim %d (built for 64 and 128)", name, a.head_dim);
+    if (a.rotary_dim < 16 || a.rotary_dim > a.head_dim || a.rotary_dim % 16)
+        return vf_fail(VF_ERR_UNSUPPORTED, "%s: rotary_dim %d of head_dim %d (multiples of 16)", name, a.rotary_dim, a.head_dim);
+    if (a.pairs != VF_ROTARY_HALF && a.pairs != VF_ROTARY_INTERLEAVED) return vf_fail(VF_ERR_ARG, "%s: pairs %d", name, a.pairs);
+    if constexpr (std::is_same<NORM, HeadNorms>::value) {
+        const vf_head_norm &n = norm.n;
+        if (!(n.eps > 0) || !std::isfinite(n.eps)) return vf_fail(VF_ERR_ARG, "%s: eps %g", name, n.eps);
+        for (const int stride : {n.q_gain_stride, n.k_gain_stride})
+            if (stride < 0 || (stride > 0 && stride < a.head_dim) || stride > 1 << 20)
+                return vf_fail(VF_ERR_ARG, "%s: gains of the heads %d elements apart", name, stride);
+        if ((n.q_gain_stride | n.k_gain_stride) & 3 || ((uintptr_t)n.q_gain_dev | (uintptr_t)n.k_gain_dev) & 15)
+            return vf_fail(VF_ERR_UNSUPPORTED, "%s: addresses and strides of gains are multiples of 16 bytes", name);
+    }
+    if (a.total_rows < 0 || a.total_rows > VF_PACKED_MAX_ROWS || a.max_positions < 1 || a.pool_pages < 1 || a.pool_pages > 0x7fffffff / VF_TILE)
+        return vf_fail(VF_ERR_ARG, "%s: %d rows, %d positions, %d pages", name, a.total_rows, a.max_positions, a.pool_pages);
+    if (a.total_rows == 0) return VF_OK;
+    if (!q_dev || !k_dev || !v_dev || !table_dev || !pos_dev || !slot_dev || !q_out_dev || !kv_layer_dev)
+        return vf_fail(VF_ERR_ARG, "%s: NULL argument", name);
+    const int es = a.dtype == VF_BF16 ? 2 : 4;
+    const int64_t wq = (int64_t)a.n_q_heads * a.head_dim, wkv = (int64_t)a.n_kv_heads * a.head_dim;
+    if (a.q_stride < wq || a.q_out_stride < wq || a.k_stride < wkv || a.v_stride < wkv)
+        return vf_fail(VF_ERR_ARG, "%s: rows overlap (strides %lld, %lld, %lld, %lld)", name, (long long)a.q_stride,
+                       (long long)a.k_stride, (long long)a.v_stride, (long long)a.q_out_stride);
+    if (q_out_dev == q_dev && a.q_out_stride != a.q_stride) return vf_fail(VF_ERR_ARG, "%s: q in place with another stride", name);
+    if (((a.q_stride | a.k_stride | a.v_stride | a.q_out_stride) * es | (int64_t)(uintptr_t)q_dev | (int64_t)(uintptr_t)k_dev |
+         (int64_t)(uintptr_t)v_dev | (int64_t)(uintptr_t)q_out_dev | (int64_t)(uintptr_t)kv_layer_dev) & 15 || (uintptr_t)table_dev & 15)
+        return vf_fail(VF_ERR_UNSUPPORTED, "%s: addresses and strides are multiples of 16 bytes", name);
+    hipStream_t st = (hipStream_t)stream;
+    const auto launch = a.dtype == VF_BF16 ? (a.head_dim == 128 ? launch_rotary<bf16_t, 128, NORM> : launch_rotary<bf16_t, 64, NORM>)
+                                           : (a.head_dim == 128 ? launch_rotary<float, 128, NORM> : launch_rotary<float, 64, NORM>);
+    return launch(name, a, norm, q_dev, k_dev, v_dev, table_dev, pos_dev, slot_dev, q_out_dev, kv_layer_dev, st);
 }
 
 }  // namespace
@@ -386,33 +473,17 @@ int vf_rotary_table(const vf_rotary_plan *plan, float *table_dev, void *stream) 
 
 int vf_rotary_append(const vf_rotary_args *args, const void *q_dev, const void *k_dev, const void *v_dev, const float *table_dev,
                      const int32_t *pos_dev, const int32_t *slot_dev, void *q_out_dev, void *kv_layer_dev, void *stream) {
-    if (!args) return vf_fail(VF_ERR_ARG, "vf_rotary_append: NULL argument");
-    const vf_rotary_args &a = *args;
-    if (a.dtype != VF_F32 && a.dtype != VF_BF16) return vf_fail(VF_ERR_ARG, "vf_rotary_append: dtype %d", a.dtype);
-    if (a.n_q_heads < 1 || a.n_kv_heads < 1 || a.n_q_heads > 256 || a.n_kv_heads > 256)
-        return vf_fail(VF_ERR_ARG, "vf_rotary_append: %d query heads, %d key heads", a.n_q_heads, a.n_kv_heads);
-    if (a.head_dim != 64 && a.head_dim != 128) return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: head_dim %d (built for 64 and 128)", a.head_dim);
-    if (a.rotary_dim < 16 || a.rotary_dim > a.head_dim || a.rotary_dim % 16)
-        return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: rotary_dim %d of head_dim %d (multiples of 16)", a.rotary_dim, a.head_dim);
-    if (a.pairs != VF_ROTARY_HALF && a.pairs != VF_ROTARY_INTERLEAVED) return vf_fail(VF_ERR_ARG, "vf_rotary_append: pairs %d", a.pairs);
-    if (a.total_rows < 0 || a.total_rows > VF_PACKED_MAX_ROWS || a.max_positions < 1 || a.pool_pages < 1 || a.pool_pages > 0x7fffffff / VF_TILE)
-        return vf_fail(VF_ERR_ARG, "vf_rotary_append: %d rows, %d positions, %d pages", a.total_rows, a.max_positions, a.pool_pages);
-    if (a.total_rows == 0) return VF_OK;
-    if (!q_dev || !k_dev || !v_dev || !table_dev || !pos_dev || !slot_dev || !q_out_dev || !kv_layer_dev)
-        return vf_fail(VF_ERR_ARG, "vf_rotary_append: NULL argument");
-    const int es = a.dtype == VF_BF16 ? 2 : 4;
-    const int64_t wq = (int64_t)a.n_q_heads * a.head_dim, wkv = (int64_t)a.n_kv_heads * a.head_dim;
-    if (a.q_stride < wq || a.q_out_stride < wq || a.k_stride < wkv || a.v_stride < wkv)
-        return vf_fail(VF_ERR_ARG, "vf_rotary_append: rows overlap (strides %lld, %lld, %lld, %lld)", (long long)a.q_stride,
-                       (long long)a.k_stride, (long long)a.v_stride, (long long)a.q_out_stride);
-    if (q_out_dev == q_dev && a.q_out_stride != a.q_stride) return vf_fail(VF_ERR_ARG, "vf_rotary_append: q in place with another stride");
-    if (((a.q_stride | a.k_stride | a.v_stride | a.q_out_stride) * es | (int64_t)(uintptr_t)q_dev | (int64_t)(uintptr_t)k_dev |
-         (int64_t)(uintptr_t)v_dev | (int64_t)(uintptr_t)q_out_dev | (int64_t)(uintptr_t)kv_layer_dev) & 15 || (uintptr_t)table_dev & 15)
-        return vf_fail(VF_ERR_UNSUPPORTED, "vf_rotary_append: addresses and strides are multiples of 16 bytes");
-    hipStream_t st = (hipStream_t)stream;
-    const auto launch = a.dtype == VF_BF16 ? (a.head_dim == 128 ? launch_rotary<bf16_t, 128> : launch_rotary<bf16_t, 64>)
-                                           : (a.head_dim == 128 ? launch_rotary<float, 128> : launch_rotary<float, 64>);
-    return launch(a, q_dev, k_dev, v_dev, table_dev, pos_dev, slot_dev, q_out_dev, kv_layer_dev, st);
+    return rotary_append("vf_rotary_append", args, NoNorms{}, q_dev, k_dev, v_dev, table_dev, pos_dev, slot_dev, q_out_dev, kv_layer_dev, stream);
+}
+
+int vf_norm_rotary_append(const vf_rotary_args *args, const vf_head_norm *norm, const void *q_dev, const void *k_dev, const void *v_dev,
+                          const float *table_dev, const int32_t *pos_dev, const int32_t *slot_dev, void *q_out_dev, void *kv_layer_dev,
+                          void *stream) {
+    if (!norm) return vf_fail(VF_ERR_ARG, "vf_norm_rotary_append: NULL argument");
+    HeadNorms norms{*norm};
+    if (!norm->q_gain_dev) norms.n.q_gain_stride = 0;
+    if (!norm->k_gain_dev) norms.n.k_gain_stride = 0;
+    return rotary_append("vf_norm_rotary_append", args, norms, q_dev, k_dev, v_dev, table_dev, pos_dev, slot_dev, q_out_dev, kv_layer_dev, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,194 @@
+"""vf_logits_adjust against the float64 oracle: penalties, biases, masks on the logits of packed rows."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_15312_amd as vf
+from oracle import packed as op
+from util_gpu import DEV, f32, i32
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _bits(mask, words=None):
+    """[rows, vocab] truth values as int32 words, bit v % 32 of word v / 32; `words` of them a row, the rest all ones."""
+    mask = np.asarray(mask, bool)
+    words = words or -(-mask.shape[1] // 32)
+    wide = np.ones((len(mask), 32 * words), bool)
+    wide[:, :mask.shape[1]] = mask
+    return torch.as_tensor(np.packbits(wide, axis=1, bitorder="little").view(np.int32), device=DEV)
+
+
+class Call:
+    """A call with the arguments that `what` names, random and with every case of ids in them."""
+
+    def __init__(self, seed, vocab, rows_of, dtype="f32", what="penalties history prompt tokens biases mask mask_row", most=300, stride=0):
+        rng = np.random.default_rng(seed)
+        what = what.split()
+        n, self.row_off = len(rows_of), np.concatenate([[0], np.cumsum(rows_of)]).astype(int)
+        self.rows = int(self.row_off[-1])
+        wide = torch.randn((max(self.rows, 1), vocab + stride), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV).mul_(5).to(TYPES[dtype])
+        self.logits = wide[:self.rows, :vocab]
+        few = lambda k: rng.choice(np.concatenate([rng.integers(0, vocab, 20), [0, vocab - 1, -1, vocab, 1 << 30, -(1 << 31)]]), k)  # noqa: E731
+        self.kw = dict(penalties=None, history=None, prompt_len=None, tokens=None, biases=None, mask=None, mask_row=None)
+        if "penalties" in what:
+            p = np.stack([rng.uniform(0.7, 1.6, n), rng.uniform(-1, 1, n), rng.uniform(-0.5, 0.5, n)], 1)
+            p[rng.random(n) < 0.2] = [1, 0, 0]
+            self.kw["penalties"] = p.astype(np.float32)
+        if "history" in what:
+            self.kw["history"] = [few(int(rng.integers(0, most + 1))) for _ in range(n)]
+        if "prompt" in what:
+            self.kw["prompt_len"] = [int(rng.integers(-1, most + 20)) for _ in range(n)]
+        if "tokens" in what:
+            self.kw["tokens"] = few(self.rows)
+        if "biases" in what:
+            self.kw["biases"] = [[(int(v), float(np.float32(x))) for v, x in zip(few(m), rng.normal(size=m) * 3)] for m in rng.integers(0, 40, n)]
+        if "mask" in what:
+            m = rng.random((self.rows + 3, vocab)) < rng.choice([0.02, 0.5, 0.98], self.rows + 3)[:, None]
+            m[0] = False                                                          # nothing is left
+            self.kw["mask"] = m
+            if "mask_row" in what:
+                self.kw["mask_row"] = rng.integers(-2, self.rows + 5, self.rows)
+
+    def device(self):
+        k = self.kw
+        d = dict(penalties=None if k["penalties"] is None else f32(k["penalties"]), tokens=None if k["tokens"] is None else i32(k["tokens"]),
+                 prompt_len=None if k["prompt_len"] is None else i32(k["prompt_len"]),
+                 mask=None if k["mask"] is None else _bits(k["mask"]), mask_row=None if k["mask_row"] is None else i32(k["mask_row"]))
+        if k["history"] is not None:
+            most = max(len(h) for h in k["history"]) + 2
+            d["history"] = i32([list(h) + [3] * (most - len(h)) for h in k["history"]])
+            d["history_len"] = i32([len(h) for h in k["history"]])
+        if k["biases"] is not None:
+            all_ = [p for b in k["biases"] for p in b]
+            d["biases"] = (i32(np.concatenate([[0], np.cumsum([len(b) for b in k["biases"]])])), i32([v for v, _ in all_]), f32([x for _, x in all_]))
+        return d
+
+    def check(self, out, row_off=None):
+        torch.cuda.synchronize()
+        row_off = self.row_off if row_off is None else row_off
+        z, got = self.before.double().cpu().numpy(), out.double().cpu().numpy()
+        want = op.logits_adjust(z, row_off, **self.kw)
+        inside = ~np.isnan(want).all(1)
+        # a division or product, alpha + beta n (product and sum), two more sums: each rounds once, by 2^-24 of what it holds
+        rho = np.ones((len(z), 1))
+        add = np.zeros((len(z), 1))
+        for b in range(len(row_off) - 1):
+            if self.kw["penalties"] is not None:
+                r, a, f = np.abs(self.kw["penalties"][b].astype(float))
+                times = (len(self.kw["history"][b]) if self.kw["history"] is not None else 0) + row_off[b + 1] - row_off[b]
+                rho[row_off[b]:row_off[b + 1]], add[row_off[b]:row_off[b + 1]] = max(r, 1 / r), a + f * times
+            if self.kw["biases"] is not None:
+                add[row_off[b]:row_off[b + 1]] += max([abs(x) for _, x in self.kw["biases"][b]], default=0)
+        bound = 2.0 ** -24 * (3 * np.abs(z) * rho + 4 * add)
+        masked = np.isneginf(want)
+        assert np.array_equal(masked[inside], np.isneginf(got[inside]))
+        fine = inside[:, None] & ~masked
+        assert (np.abs(got - want)[fine] <= bound[fine]).all()
+        return inside
+
+    def run(self, in_place=False, out_stride=0):
+        self.before = self.logits.clone()
+        wide = torch.full((max(self.rows, 1), self.logits.shape[1] + out_stride), 7.0, device=DEV)
+        out = self.logits if in_place else wide[:self.rows, :self.logits.shape[1]]
+        vf.vf_logits_adjust(self.logits, i32(self.row_off), out, **self.device())
+        assert self.check(out).all()
+        assert in_place or (wide[:, self.logits.shape[1]:] == 7).all()
+        assert in_place or torch.equal(self.before, self.logits)
+
+
+EVERY = "penalties history prompt tokens biases mask mask_row"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,rows_of", [(1, [1]), (31, [2, 0, 1]), (32, [1, 1]), (1000, [5]), (2048, [1, 33]), (2052, [3, 3]), (4097, [17]), (4096, [1] * 70),
+                                          (151936, [2, 9]), (10001, [33, 0, 0, 1, 20])])
+def test_everything_at_once(vocab, rows_of, dtype):
+    Call(vocab, vocab, rows_of, dtype).run()
+
+
+@pytest.mark.parametrize("what", ["", "penalties", "penalties history", "penalties history prompt", "penalties tokens", "biases", "mask", "mask mask_row",
+                                  "history prompt tokens", "penalties biases", "tokens biases mask"])
+@pytest.mark.parametrize("vocab", [5000, 5003])
+def test_arguments_that_are_left_out(vocab, what):
+    Call(7, vocab, [1, 4, 0, 2], what=what).run()
+
+
+@pytest.mark.parametrize("vocab,stride", [(4096, 0), (4099, 0), (4096, 3), (4099, 5), (3000, 8)])
+def test_in_place(vocab, stride):
+    Call(11, vocab, [4, 1, 30], stride=stride).run(in_place=True)
+
+
+@pytest.mark.parametrize("stride,out_stride", [(4, 8), (1, 0), (0, 2), (12, 4)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_apart(dtype, stride, out_stride):
+    Call(13, 6000, [3, 2], dtype, stride=stride).run(out_stride=out_stride)
+
+
+def test_a_start_that_is_not_aligned():
+    for shift in (1, 2, 3, 4):
+        c = Call(17, 4096, [2, 5], stride=8)
+        wide = torch.full((c.rows, 4112), 7.0, device=DEV)
+        c.before = c.logits.clone()
+        vf.vf_logits_adjust(c.logits, i32(c.row_off), wide[:, shift:shift + 4096], **c.device())
+        assert c.check(wide[:, shift:shift + 4096]).all() and (wide[:, :shift] == 7).all() and (wide[:, shift + 4096:] == 7).all()
+
+
+def test_many_rows_a_workgroup():
+    """So many rows that a workgroup has several, of several sequences; long histories."""
+    Call(19, 4100, [1, 0, 33, 2, 2, 1] * 300, "bf16", most=3000).run()
+    Call(23, 66000, [40, 1, 300], most=9000).run()
+
+
+def test_no_rows_and_rows_outside():
+    Call(29, 100, [0, 0]).run()
+    c = Call(31, 5000, [3, 4, 2])
+    for row_off in ([2, 5, 5, 8], [0, 0, 0, 0], [4, 4, 9, 9], [1, 1, 2, 2]):
+        c.before, out = c.logits.clone(), torch.full(c.logits.shape, 7.0, device=DEV)
+        vf.vf_logits_adjust(c.logits, i32(row_off), out, **c.device())
+        inside = c.check(out, row_off)
+        assert inside.sum() == row_off[-1] - row_off[0] and (out[torch.as_tensor(~inside, device=DEV)] == 7).all()
+
+
+def test_sequences_of_a_full_batch():
+    rng = np.random.default_rng(2)
+    Call(37, 50, rng.integers(0, 3, 4096).tolist(), most=5).run()
+
+
+def test_values_that_are_not_finite():
+    vocab = 2051
+    z = torch.randn((2, vocab), device=DEV)
+    z[:, 5], z[:, 6], z[:, 7], z[:, 8], z[:, 9] = float("nan"), float("inf"), -float("inf"), -0.0, torch.finfo(torch.float32).min
+    out, mask = torch.empty_like(z), np.ones((1, vocab), bool)
+    mask[0, 5] = mask[0, 6] = False
+    args = dict(penalties=f32([[1.5, 0.5, 0.25]]), history=i32([[5, 6, 7, 8, 9, 9]]), history_len=i32([6]),
+                biases=(i32([0, 2]), i32([7, 9]), f32([4.0, -float("inf")])), mask=_bits(mask), mask_row=i32([0, -1]))
+    vf.vf_logits_adjust(z, i32([0, 2]), out, **args)
+    out = out.cpu().numpy()
+    assert np.isneginf(out[0, 5]) and np.isneginf(out[0, 6])                     # masked, whatever was there
+    assert np.isnan(out[1, 5]) and np.isposinf(out[1, 6]) and np.isneginf(out[:, 7]).all() and np.isneginf(out[:, 9]).all()
+    assert (out[:, 8] == -0.75).all()
+    assert np.array_equal(out[:, 10:], z[:, 10:].cpu().numpy())
+
+
+def test_lengths_outside_the_history():
+    """Lengths past the room of a history are cut, negative ones are none; offsets of biases past the list are cut."""
+    vocab, z = 300, torch.ones((3, 300), device=DEV)
+    out = torch.empty_like(z)
+    vf.vf_logits_adjust(z, i32([0, 1, 2, 3]), out, penalties=f32([[2.0, 0, 0]] * 3), history=i32([[4, 5], [6, 7], [8, 9]]), history_len=i32([99, -2, 1]),
+                        prompt_len=i32([50, 1, -9]), biases=(i32([-5, 1, 1, 77]), i32([1, 2]), f32([10.0, 20.0])))
+    want = np.ones((3, vocab))
+    want[0, [4, 5]], want[2, 8], want[0, 1], want[2, 2] = 0.5, 0.5, 11.0, 21.0
+    assert np.array_equal(out.cpu().numpy(), want)
+
+
+def test_a_row_past_32_bits():
+    """Rows that start more than 2^31 elements behind the first."""
+    vocab, rows = 151936, 14400
+    z = torch.zeros((rows, vocab), dtype=torch.bfloat16, device=DEV)
+    z[-1, -1], z[-1, 0] = 3.0, -2.0
+    out = torch.empty((rows, vocab), dtype=torch.float32, device=DEV)
+    vf.vf_logits_adjust(z, i32([0, rows - 1, rows]), out, penalties=f32([[1, 0, 0], [2.0, 0, 0]]), tokens=torch.zeros(rows, dtype=torch.int32, device=DEV),
+                        biases=(i32([0, 0, 1]), i32([vocab - 1]), f32([1.5])))
+    assert out[-1, 0] == -4.0 and out[-1, -1] == 4.5 and not out[-2].any() and not out[:, 1:-1].any()

@@ -651,12 +651,16 @@ def vf_pages_compact(lens, block_table, shares, table_out, shares_out, free_out,
 
 
 def _layers(name, t, dev):
-    """(layers, pages, bytes a page, bytes between layers) of pages [layers, pages, ...] or of one layer's, [pages, 2, kv heads, 64 * hd]."""
-    if t.dim() == 4:
-        t = t[None]
-    if t.dim() != 5 or not t.is_cuda or not t[0].is_contiguous() or dev is not None and t.get_device() != dev:
-        _refuse(f"{name}: tensor [layers, pages, 2, kv heads, 64 * head_dim] whose layers are contiguous{_on(dev)}")
-    return t.shape[0], t.shape[1], t[0, 0].numel() * t.element_size(), t.stride(0) * t.element_size()
+    """(layers, pages, bytes a page, bytes between layers) of pages [layers, pages, 2, kv heads, 64 * hd], or of one layer's without the first."""
+    shape, stride, size = t.shape, t.stride(), 1
+    if not 4 <= len(shape) <= 5 or not t.is_cuda or dev is not None and t.get_device() != dev:
+        _refuse(f"{name}: tensor [layers, pages, 2, kv heads, 64 * head_dim]{_on(dev)}")
+    for n, step in zip(shape[:-5:-1], stride[:-5:-1]):
+        if step != size and n > 1:
+            _refuse(f"{name}: layers that are contiguous")
+        size *= n
+    es, layers = t.element_size(), shape[0] if len(shape) == 5 else 1
+    return layers, shape[-4], size // max(shape[-4], 1) * es, (stride[0] if layers > 1 else size) * es
 
 
 def vf_pages_copy(pools, copies, n_copies, to):

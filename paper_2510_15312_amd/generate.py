@@ -3,25 +3,79 @@
 Every piece of work is a call of the C ABI: chunked prefill (`vf_prefill_chunk`), the retrieval
 drafter over the text so far (`vf_draft_suffix_match`), the pool of reusable rejected drafts
 (`vf_reuse_pool_*`), the verify forward (`vf_verify`), acceptance (`vf_accept`) and the reuse
-segment (`vf_reuse_select`).  This module only strings them together and moves the few integers a
+segment (`vf_reuse_select`), with `vf_logits_adjust` between the two where the logits are to be adjusted.  This module only strings them together and moves the few integers a
 step decides (accepted count, emitted tokens, reuse segment) to the host, once per step.
 """
+import numpy as np
 import torch
 
 from . import binding as vf
 
 
-def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=256, reuse_max_age=2, drafter=None, reuse=True):
+class _Adjust:
+    """What `generate` puts on the logits: the text so far on the device, biases, and the masks of a step's rows."""
+
+    def __init__(self, penalties, biases, allowed, prompt, room, vocab, dev):
+        ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+        self.allowed, self.vocab, self.dev, self.ints = allowed, vocab, dev, ints
+        self.logits = torch.empty((vf.VF_MAX_DRAFTS + 1, vocab), dtype=torch.float32, device=dev)
+        self.more = {}
+        if penalties is not None:
+            self.more = dict(penalties=torch.tensor([list(penalties)], dtype=torch.float32, device=dev), prompt_len=ints([len(prompt)]),
+                             history=torch.zeros((1, room), dtype=torch.int32, device=dev), history_len=ints([0]))
+        if biases:
+            self.more["biases"] = (ints([0, len(biases)]), ints(list(biases)), torch.tensor(list(biases.values()), dtype=torch.float32, device=dev))
+        self.length = 0
+
+    def __call__(self, text, tokens, drafts):
+        """The logits of the rows of the text's end and of the drafts behind it, in place.  tokens: the rows' tokens on the device;
+        the first of them, the pending token, counts as the end of the text."""
+        m, more = len(drafts) + 1, dict(self.more)
+        if "history" in more:
+            more["history"][0, self.length:len(text)] = self.ints(text[self.length:])
+            more["history_len"].fill_(len(text))
+            self.length = len(text)
+            more["tokens"] = tokens
+        if self.allowed is not None:
+            bits, rows = np.zeros((m, -(-self.vocab // 32) * 32), bool), [-1] * m
+            for i in range(m):
+                ids = self.allowed(list(text) + list(drafts[:i]))
+                if ids is not None:
+                    ids = [int(v) for v in ids]
+                    if not all(0 <= v < self.vocab for v in ids):
+                        raise ValueError(f"allowed ids outside the vocabulary of {self.vocab}")
+                    bits[i, ids], rows[i] = True, i
+            words = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32))
+            more.update(mask=words.to(self.dev), mask_row=self.ints(rows))
+        vf.vf_logits_adjust(self.logits[:m], self.ints([0, m]), self.logits[:m], **more)
+        return self.logits[:m]
+
+
+def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=256, reuse_max_age=2, drafter=None, reuse=True,
+             penalties=None, biases=None, allowed=None):
     """prompt: host ints; returns (the n_new generated tokens, statistics).  Greedy acceptance: the
     result is what plain greedy decoding would produce.  drafter(text, k) -> list of at most k draft
     ids replaces the library's suffix-match drafter (any drafter gives the same text); reuse=False
-    leaves the pool of rejected drafts out."""
+    leaves the pool of rejected drafts out.
+
+    The logits are adjusted before a token is taken from them (`vf_logits_adjust`), so that the text is what plain greedy
+    decoding with the same adjustments would produce: penalties (repetition, presence, frequency); biases {id: value};
+    allowed(text) -> the ids that may follow a text, prompt included, or None for all."""
     dev = model.buf.device
     k = min(int(k), vf.VF_MAX_DRAFTS)
     toks = torch.as_tensor(list(prompt), dtype=torch.int32, device=dev)
+    adjust = None
+    if penalties is not None or biases or allowed is not None:
+        adjust = _Adjust(penalties, biases, allowed, prompt, len(prompt) + n_new + vf.VF_MAX_DRAFTS + 1, model.cfg.vocab, dev)
     for c0 in range(0, len(prompt), chunk):
-        vf.vf_prefill_chunk(model, seq, toks[c0:c0 + chunk], sample_first=c0 + chunk >= len(prompt))
+        last = c0 + chunk >= len(prompt)
+        vf.vf_prefill_chunk(model, seq, toks[c0:c0 + chunk], sample_first=last, logits_mode=int(last and adjust is not None),
+                            logits_out=adjust.logits if last and adjust is not None else None)
     length, pending = vf.vf_seq_get_state(seq)
+    if adjust is not None:                              # the first token comes from adjusted logits too
+        z = adjust([int(t) for t in prompt], None, [])[0]
+        pending = int((z == z.max()).nonzero()[0])      # the lowest of equal ones, as vf_accept has it
+        vf.vf_seq_set_pending(seq, pending)
     text = [int(t) for t in prompt] + [pending]        # the pending token is the first generated one
     pool = vf.vf_reuse_pool_init(reuse_max_age, max(k, 1))
     n_acc = torch.zeros(1, dtype=torch.int32, device=dev)
@@ -40,8 +94,13 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
         drafts = vf.vf_reuse_pool_extend(pool, fresh) if k and reuse else fresh
         m = len(drafts) + 1
         tokens = torch.as_tensor([vf.VF_PENDING] + drafts, dtype=torch.int32, device=dev)
-        vf.vf_verify(model, [seq], tokens, [0, m])
-        vf.vf_accept(model, [seq], tokens, [0, m], greedy, n_acc, out[:m], y[:m])
+        logits = None
+        if adjust is None:
+            vf.vf_verify(model, [seq], tokens, [0, m])
+        else:
+            vf.vf_verify(model, [seq], tokens, [0, m], adjust.logits)
+            logits = adjust(text, tokens, drafts)
+        vf.vf_accept(model, [seq], tokens, [0, m], greedy, n_acc, out[:m], y[:m], logits)
         if drafts and reuse:
             vf.vf_reuse_select(tokens, [0, m], y[:m], n_acc, seg)
         host = torch.cat([n_acc, seg, out[:m]]).cpu().tolist()          # the step's one synchronisation

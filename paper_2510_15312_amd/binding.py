@@ -652,15 +652,14 @@ def vf_pages_compact(lens, block_table, shares, table_out, shares_out, free_out,
 
 def _layers(name, t, dev):
     """(layers, pages, bytes a page, bytes between layers) of pages [layers, pages, 2, kv heads, 64 * hd], or of one layer's without the first."""
-    shape, stride, size = t.shape, t.stride(), 1
+    shape, stride, es = t.shape, t.stride(), t.element_size()
     if not 4 <= len(shape) <= 5 or not t.is_cuda or dev is not None and t.get_device() != dev:
         _refuse(f"{name}: tensor [layers, pages, 2, kv heads, 64 * head_dim]{_on(dev)}")
-    for n, step in zip(shape[:-5:-1], stride[:-5:-1]):
-        if step != size and n > 1:
-            _refuse(f"{name}: layers that are contiguous")
-        size *= n
-    es, layers = t.element_size(), shape[0] if len(shape) == 5 else 1
-    return layers, shape[-4], size // max(shape[-4], 1) * es, (stride[0] if layers > 1 else size) * es
+    pages, a, b, c = shape[-4:]
+    if stride[-4:] != (a * b * c, b * c, c, 1) and any(n > 1 and step != want for n, step, want in zip(shape[-4:], stride[-4:], (a * b * c, b * c, c, 1))):
+        _refuse(f"{name}: layers that are contiguous")
+    layers = shape[0] if len(shape) == 5 else 1
+    return layers, pages, a * b * c * es, (stride[0] if layers > 1 else pages * a * b * c) * es
 
 
 def vf_pages_copy(pools, copies, n_copies, to):
@@ -668,8 +667,8 @@ def vf_pages_copy(pools, copies, n_copies, to):
     copies int32 [any, 2], n_copies int32 [1] on the device."""
     dev = _device("pools", pools)
     layers, pages, size, stride = _layers("pools", pools, dev)
-    to_layers, to_pages, to_size, to_stride = _layers("to", to, dev)
-    if (to_layers, to_size) != (layers, size) or to.dtype is not pools.dtype:
+    to_layers, to_pages, to_size, to_stride = (layers, pages, size, stride) if to is pools else _layers("to", to, dev)
+    if to_layers != layers or to_size != size or to.dtype is not pools.dtype:
         _refuse("pools of other layers, heads or types")
     a = vf_copy_args(layers, size, pages, to_pages, copies.numel() // 2, 0, stride, to_stride)
     _check(lib.vf_pages_copy(C.byref(a), pools.data_ptr(), to.data_ptr(), _ints("copies", copies, 0, dev), _ints("n_copies", n_copies, 1, dev),
@@ -679,14 +678,12 @@ def vf_pages_copy(pools, copies, n_copies, to):
 # ---- logits ----------------------------------------------------------------------------------------
 
 def _matrix(name, t, dtype, rows, columns, dev):
-    """The row stride of a device tensor [rows, columns] whose rows are contiguous; None for any number stands for any."""
-    if t.dim() != 2 or t.dtype is not dtype or not t.is_cuda or dev is not None and t.get_device() != dev or \
-            rows is not None and t.shape[0] != rows or columns is not None and t.shape[1] != columns:
-        _refuse(f"{name}: tensor [{'any' if rows is None else rows}, {'any' if columns is None else columns}] of {dtype}{_on(dev)}")
-    row, one = t.stride()
-    if one != 1 and t.shape[1] > 1:
-        _refuse(f"{name}: rows that are contiguous")
-    return row if t.shape[0] > 1 else max(row, t.shape[1])
+    """The row stride of a device tensor [rows, columns] whose rows are contiguous; rows or columns None: any number."""
+    s, steps = t.shape, t.stride()
+    if len(s) != 2 or t.dtype is not dtype or not t.is_cuda or rows is not None and s[0] != rows or columns is not None and s[1] != columns or \
+            steps[1] != 1 and s[1] > 1 or dev is not None and t.get_device() != dev:
+        _refuse(f"{name}: tensor [{'any' if rows is None else rows}, {'any' if columns is None else columns}] of {dtype}, rows that are contiguous{_on(dev)}")
+    return steps[0] if s[0] > 1 else max(steps[0], s[1])
 
 
 def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history_len=None, prompt_len=None, tokens=None, biases=None,
@@ -695,31 +692,35 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
     penalties float32 [n, 3] (repetition, presence, frequency), history int32 [n, any], history_len and prompt_len int32 [n], tokens
     int32 [rows], biases: int32 offsets [n + 1], int32 ids and float32 values [any]; mask int32 [any, at least vocab / 32] (a bit an id),
     mask_row int32 [rows].  What is None is left out."""
-    dev = _device("logits", logits)
-    if logits.dim() != 2:
+    dev, shape, n = _device("logits", logits), logits.shape, row_off.numel() - 1
+    if len(shape) != 2:
         _refuse(f"logits: tensor [rows, vocab]{_on(dev)}")
-    (rows, vocab), n = logits.shape, row_off.numel() - 1
+    rows, vocab = shape
     in_stride, out_stride = _matrix("logits", logits, logits.dtype, rows, vocab, dev), _matrix("out", out, torch.float32, rows, vocab, dev)
 
-    def ints(name, t, k):
-        return None if t is None else _ints(name, t, k, dev)
-    a = vf_logits_args(_dtype(logits), n, rows, vocab, 0, 0, 0, 0, in_stride, out_stride, 0, 0)
-    if penalties is not None and (_matrix("penalties", penalties, torch.float32, n, 3, dev) != 3):
-        _refuse(f"penalties: contiguous float32 tensor [{n}, 3]{_on(dev)}")
+    penalty = text = bits = None
+    text_most = text_stride = masks = mask_stride = entries = 0
+    if penalties is not None:
+        if _matrix("penalties", penalties, torch.float32, n, 3, dev) != 3:
+            _refuse(f"penalties: contiguous float32 tensor [{n}, 3]{_on(dev)}")
+        penalty = penalties.data_ptr()
     if history is not None:
-        a.history_stride, a.max_history = _matrix("history", history, _I32, n, None, dev), history.shape[1]
+        text_stride, text_most, text = _matrix("history", history, _I32, n, None, dev), history.shape[1], history.data_ptr()
     if mask is not None:
-        a.mask_stride, a.mask_rows = _matrix("mask", mask, _I32, None, None, dev), mask.shape[0]
-        if 32 * mask.shape[1] < vocab or mask_row is None and mask.shape[0] < rows:
+        mask_stride, bits, (masks, words) = _matrix("mask", mask, _I32, None, None, dev), mask.data_ptr(), mask.shape
+        if 32 * words < vocab or mask_row is None and masks < rows:
             _refuse(f"mask: a bit for each of {vocab} ids, and a row for each row without mask_row")
-    bias_off, bias_id, bias = biases if biases is not None else (None, None, None)
-    if bias_off is not None:
-        a.bias_entries = bias_id.numel()
-        if bias.dtype is not torch.float32 or not bias.is_cuda or not bias.is_contiguous() or bias.numel() != a.bias_entries or \
+    bias_off = bias_id = bias = None
+    if biases is not None:
+        bias_off, bias_id, bias = biases
+        entries = bias_id.numel()
+        if bias.dtype is not torch.float32 or not bias.is_cuda or not bias.is_contiguous() or bias.numel() != entries or \
                 dev is not None and bias.get_device() != dev:
-            _refuse(f"biases: contiguous float32 tensor of {a.bias_entries} entries{_on(dev)}")
-    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    _check(lib.vf_logits_adjust(C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), address(penalties), address(history),
-                                ints("history_len", history_len, n), ints("prompt_len", prompt_len, n), ints("tokens", tokens, rows),
-                                ints("bias_off", bias_off, n + 1), ints("bias_id", bias_id, 0), address(bias), address(mask),
-                                ints("mask_row", mask_row, rows), _stream_of(logits)))
+            _refuse(f"biases: contiguous float32 tensor of {entries} entries{_on(dev)}")
+        bias_off, bias_id, bias = _ints("bias_off", bias_off, n + 1, dev), _ints("bias_id", bias_id, 0, dev), bias.data_ptr()
+    a = vf_logits_args(_dtype(logits), n, rows, vocab, text_most, entries, masks, 0, in_stride, out_stride, text_stride, mask_stride)
+    _check(lib.vf_logits_adjust(C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), penalty, text,
+                                None if history_len is None else _ints("history_len", history_len, n, dev),
+                                None if prompt_len is None else _ints("prompt_len", prompt_len, n, dev),
+                                None if tokens is None else _ints("tokens", tokens, rows, dev), bias_off, bias_id, bias, bits,
+                                None if mask_row is None else _ints("mask_row", mask_row, rows, dev), _stream_of(logits)))

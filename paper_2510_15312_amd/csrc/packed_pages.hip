@@ -139,23 +139,46 @@ struct KeepArgs {
 };
 
 __device__ __forceinline__ int now(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// A barrier behind which the workgroup's atomics have been done.
+__device__ __forceinline__ void done() {
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __syncthreads();
+}
 
 // One workgroup, whose barriers separate the steps: (1) every table entry behind what its sequence keeps drops its hold of its page
 // (shares - 1); (2) a page that nobody holds any more (shares < 0) goes on the free list where the first entry that named it stands;
 // (3) sequences cut inside a page that others hold drop their hold of it too and get a page of their own, but for the last of them
 // where nobody else is left.  Counts are added up with atomics, whose order does not matter; who is first or last is settled by a
-// minimum over the entries' numbers, kept in the (negative) count itself.  That step is left out where no page was dropped twice.
+// minimum over the entries' numbers, kept in the (negative) count itself.  That step is left out where no page was dropped twice, and
+// the third where no sequence is cut inside a page.
+// What bounds it is the way from one step to the next, a trip to the L2 each, so a thread keeps the pages of its entries and of its sequences
+// (of the first LIST_THREADS * LIST_ENTRIES; more are read again).
 __global__ __launch_bounds__(LIST_THREADS) void pages_keep_kernel(KeepArgs a) {
     extern __shared__ int lds[];
     const PagesArgs &p = a.p;
     const int tid = threadIdx.x, n = p.n_seqs;
     int *start = lds, *first = lds + n + 1;     // entries that go before sequence b's; the first page that it drops
-    __shared__ int wave_sums[LIST_THREADS / 64], twice;
+    __shared__ int wave_sums[LIST_THREADS / 64], twice, cuts;
     constexpr int FIRST = -0x7fffffff - 1;      // a count that names entry e: FIRST + e
-    if (tid == 0) start[0] = twice = 0;
-    int gone = 0;
-    for (int b0 = 0; b0 < n; b0 += LIST_THREADS) {
-        const int b = b0 + tid, h = b < n ? held_of(a.len[b], p) : 0, w = b < n ? a.keep[b] : -1, k = w < 0 || w > h ? h : w;
+    constexpr int EACH = VF_PACKED_MAX_SEQS / LIST_THREADS;
+    if (tid == 0) start[0] = twice = cuts = 0;
+    int gone = 0, n_free = min(max(a.n_free[0], 0), p.free_entries);
+    int kept[EACH], cut[EACH];                  // sequence tid + i * LIST_THREADS: what it keeps; the page that it is cut inside, or -1
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        kept[i] = 0;
+        cut[i] = -1;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (i * LIST_THREADS >= n) break;
+        const int b = tid + i * LIST_THREADS;
+        const int h = b < n ? held_of(a.len[b], p) : 0, w = b < n ? a.keep[b] : -1, k = w < 0 || w > h ? h : w;
+        if (b < n && k < h && k % VF_TILE) {
+            cut[i] = a.table[(size_t)b * p.table_stride + k / VF_TILE];
+            if (!in_pool(cut[i], p)) cut[i] = -1;
+        }
+        kept[i] = k;
         int total;
         const int upto = gone + scan<LIST_THREADS>(pages_of(h) - pages_of(k), wave_sums, total);
         gone += total;
@@ -163,45 +186,57 @@ __global__ __launch_bounds__(LIST_THREADS) void pages_keep_kernel(KeepArgs a) {
             start[b + 1] = upto;
             first[b] = pages_of(k);
         }
+        if (cut[i] >= 0) cuts = 1;
     }
     __syncthreads();
-    auto entry = [&](int e) {
-        const int b = last_not_above(start, n + 1, e);
-        return a.table + (size_t)b * p.table_stride + first[b] + (e - start[b]);
-    };
-    for (int e0 = tid; e0 < gone; e0 += LIST_THREADS * LIST_ENTRIES) {
-        int page[LIST_ENTRIES];
+    constexpr int CHUNK = LIST_THREADS * LIST_ENTRIES;
+    int page[LIST_ENTRIES];                     // of the entries e0 + tid * LIST_ENTRIES + i
+    int32_t *entry[LIST_ENTRIES];
+    auto pages_from = [&](int e0) {
+        const int e1 = e0 + tid * LIST_ENTRIES;
+        int b = e1 < gone ? last_not_above(start, n + 1, e1) : n;
 #pragma unroll
-        for (int i = 0; i < LIST_ENTRIES; ++i) page[i] = e0 + i * LIST_THREADS < gone ? *entry(e0 + i * LIST_THREADS) : -1;
+        for (int i = 0; i < LIST_ENTRIES; ++i) {
+            while (b < n && e1 + i >= start[b + 1]) ++b;
+            entry[i] = b < n ? a.table + (size_t)b * p.table_stride + first[b] + (e1 + i - start[b]) : nullptr;
+        }
+#pragma unroll
+        for (int i = 0; i < LIST_ENTRIES; ++i) page[i] = entry[i] ? *entry[i] : -1;
+#pragma unroll
+        for (int i = 0; i < LIST_ENTRIES; ++i)
+            if (!in_pool(page[i], p)) page[i] = -1;
+    };
+    for (int e0 = 0; e0 < gone; e0 += CHUNK) {
+        pages_from(e0);
         int shared = 0;
 #pragma unroll
         for (int i = 0; i < LIST_ENTRIES; ++i)
-            if (in_pool(page[i], p)) shared |= atomicSub(&a.shares[page[i]], 1);
+            if (page[i] >= 0) shared |= atomicSub(&a.shares[page[i]], 1);
         if (shared) twice = 1;      // a page that others hold, or that another entry has dropped
     }
-    __syncthreads();
-    const bool settle = twice;
+    done();
+    const bool settle = twice, again = gone > CHUNK;
     if (settle) {
-        for (int e = tid; e < gone; e += LIST_THREADS) {
-            const int page = *entry(e);
-            if (in_pool(page, p) && now(&a.shares[page]) < 0) atomicMin(&a.shares[page], FIRST + e);
+        for (int e0 = 0; e0 < gone; e0 += CHUNK) {
+            if (again) pages_from(e0);
+            int s[LIST_ENTRIES];
+#pragma unroll
+            for (int i = 0; i < LIST_ENTRIES; ++i) s[i] = page[i] >= 0 ? now(&a.shares[page[i]]) : 0;
+#pragma unroll
+            for (int i = 0; i < LIST_ENTRIES; ++i)
+                if (s[i] < 0) atomicMin(&a.shares[page[i]], FIRST + e0 + tid * LIST_ENTRIES + i);
         }
-        __syncthreads();
+        done();
     }
-    int n_free = min(max(a.n_free[0], 0), p.free_entries);
-    for (int e0 = 0; e0 < gone; e0 += LIST_THREADS * LIST_ENTRIES) {
-        int page[LIST_ENTRIES], mine = 0;
+    for (int e0 = 0; e0 < gone; e0 += CHUNK) {
+        if (again) pages_from(e0);
+        int s[LIST_ENTRIES], mine = 0;
+#pragma unroll
+        for (int i = 0; i < LIST_ENTRIES; ++i) s[i] = page[i] >= 0 ? now(&a.shares[page[i]]) : 0;
 #pragma unroll
         for (int i = 0; i < LIST_ENTRIES; ++i) {
-            const int e = e0 + tid * LIST_ENTRIES + i;
-            int32_t *at = e < gone ? entry(e) : nullptr;
-            page[i] = at ? *at : -1;
-            if (at) *at = -1;
-        }
-#pragma unroll
-        for (int i = 0; i < LIST_ENTRIES; ++i) {
-            const int s = in_pool(page[i], p) ? now(&a.shares[page[i]]) : 0;
-            if (s >= 0 || (settle && s != FIRST + e0 + tid * LIST_ENTRIES + i)) page[i] = -1;
+            if (entry[i]) *entry[i] = -1;
+            if (s[i] >= 0 || (settle && s[i] != FIRST + e0 + tid * LIST_ENTRIES + i)) page[i] = -1;
             else ++mine;
         }
         int total, at = n_free + scan<LIST_THREADS>(mine, wave_sums, total) - mine;     // (no page is reset before all have looked)
@@ -213,53 +248,48 @@ __global__ __launch_bounds__(LIST_THREADS) void pages_keep_kernel(KeepArgs a) {
                 if (at < p.free_entries) a.free_pages[at] = page[i];
                 ++at;
             }
-        __syncthreads();
+        if (again) done();
     }
     n_free = min(n_free, p.free_entries);
-    __syncthreads();
-    // sequences that are cut inside a page
-    auto cut_page = [&](int b, int &k) {    // the page, -1 where there is none or nothing to do
-        const int h = held_of(a.len[b], p), w = a.keep[b];
-        k = w < 0 || w > h ? h : w;
-        if (k == h || k % VF_TILE == 0) return -1;
-        const int page = a.table[(size_t)b * p.table_stride + k / VF_TILE];
-        return in_pool(page, p) ? page : -1;
-    };
-    for (int b = tid, k; b < n; b += LIST_THREADS)
-        if (const int page = cut_page(b, k); page >= 0) atomicSub(&a.shares[page], 1);
-    __syncthreads();
-    for (int b = tid, k; b < n; b += LIST_THREADS)
-        if (const int page = cut_page(b, k); page >= 0 && now(&a.shares[page]) < 0) atomicMin(&a.shares[page], FIRST + (n - 1 - b));
-    __syncthreads();
     int copied = 0;
-    for (int b0 = 0; b0 < n; b0 += LIST_THREADS) {
-        const int b = b0 + tid;
-        int k = 0, page = b < n ? cut_page(b, k) : -1;
-        const bool stays = page >= 0 && now(&a.shares[page]) == FIRST + (n - 1 - b);
-        const bool copies = page >= 0 && !stays;
-        int total;
-        const int upto = copied + scan<LIST_THREADS>(copies, wave_sums, total);
-        copied += total;
-        if (stays) first[b] = -1 - page;    // put back when all have looked
-        if (b < n) {
-            int kept = k;
+    if (cuts) {
+        done();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (cut[i] >= 0) atomicSub(&a.shares[cut[i]], 1);
+        done();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (cut[i] >= 0 && now(&a.shares[cut[i]]) < 0) atomicMin(&a.shares[cut[i]], FIRST + (n - 1 - (tid + i * LIST_THREADS)));
+        done();
+        bool stays[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) stays[i] = cut[i] >= 0 && now(&a.shares[cut[i]]) == FIRST + (n - 1 - (tid + i * LIST_THREADS));
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (i * LIST_THREADS >= n) break;
+            const bool copies = cut[i] >= 0 && !stays[i];
+            if (stays[i]) a.shares[cut[i]] = 0;
+            int total;
+            const int upto = copied + scan<LIST_THREADS>(copies, wave_sums, total);
+            copied += total;
             if (copies) {
                 const bool room = upto <= n_free;
                 const int to = room ? a.free_pages[n_free - upto] : -1;
-                a.table[(size_t)b * p.table_stride + k / VF_TILE] = to;
+                a.table[(size_t)(tid + i * LIST_THREADS) * p.table_stride + kept[i] / VF_TILE] = to;
                 if (room) {
-                    a.copies[2 * (upto - 1)] = page;
+                    a.copies[2 * (upto - 1)] = cut[i];
                     a.copies[2 * (upto - 1) + 1] = to;
                 } else {
-                    kept = k / VF_TILE * VF_TILE;
+                    kept[i] = kept[i] / VF_TILE * VF_TILE;
                 }
             }
-            a.kv_len[b] = kept;
         }
     }
-    __syncthreads();
-    for (int b = tid; b < n; b += LIST_THREADS)
-        if (first[b] < 0) a.shares[-1 - first[b]] = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (tid + i * LIST_THREADS < n) a.kv_len[tid + i * LIST_THREADS] = kept[i];
     if (tid == 0) {
         const int used = min(copied, n_free);
         a.n_copies[0] = used;
@@ -354,7 +384,7 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(vf_copy_args a, const c
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const uint4v *>(s + j * 4096);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4v *>(d + j * 4096) = x[j];
+            for (int j = 0; j < 4; ++j) __builtin_nontemporal_store(x[j], reinterpret_cast<uint4v *>(d + j * 4096));
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)

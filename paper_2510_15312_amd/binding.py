@@ -555,6 +555,19 @@ def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HAL
                                 pool.data_ptr(), _stream_of(q)))
 
 
+def _current_device():
+    return torch.cuda.current_device()
+
+
+def _launch(dev, call, *args):
+    """A call whose tensors are on device dev: where that is not the current one, it is for the call, as the default streams of all
+    devices have one address."""
+    if dev is None or dev == _current_device():
+        return _check(call(*args))
+    with torch.cuda.device(dev):
+        _check(call(*args))
+
+
 def _gain(name, t, heads, hd, dev):
     """(address, stride between heads) of gains [hd] or [heads, hd]; None: no gains."""
     if t is None:
@@ -572,9 +585,9 @@ def vf_norm_rotary_append(q, k, v, q_gain, k_gain, eps, table, pos, slot, q_out,
     args = _rotary_args(q, k, v, table, q_out, pool, pairs, dev)
     (qg, qs), (kg, ks) = _gain("q_gain", q_gain, args.n_q_heads, args.head_dim, dev), _gain("k_gain", k_gain, args.n_kv_heads, args.head_dim, dev)
     norm = vf_head_norm(qg, kg, qs, ks, eps, 0)
-    _check(lib.vf_norm_rotary_append(C.byref(args), C.byref(norm), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                     _ints("pos", pos, args.total_rows, dev), _ints("slot", slot, args.total_rows, dev),
-                                     q_out.data_ptr(), pool.data_ptr(), _stream_of(q)))
+    _launch(dev, lib.vf_norm_rotary_append, C.byref(args), C.byref(norm), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+            _ints("pos", pos, args.total_rows, dev), _ints("slot", slot, args.total_rows, dev),
+            q_out.data_ptr(), pool.data_ptr(), _stream_of(q))
 
 
 def _packed_args(q, pool, block_table, out, max_rows, max_keys, scale, dev):
@@ -618,11 +631,11 @@ def vf_pages_fork(src, dst, tokens, lens, free_pages, n_free, block_table, share
     pages]; results kv_len [n], n_free_out [1], copies [forks, 2], n_copies [1], and what changes in block_table and shares."""
     dev = _device("lens", lens)
     a, forks = _pages_args(block_table, shares, free_pages.numel(), dev), src.numel()
-    _check(lib.vf_pages_fork(C.byref(a), forks, _ints("src", src, forks, dev), _ints("dst", dst, forks, dev), _ints("tokens", tokens, forks, dev),
-                             _ints("lens", lens, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev),
-                             block_table.data_ptr(), _ints("shares", shares, 1, dev), _ints("kv_len", kv_len, a.n_seqs, dev),
-                             _ints("n_free_out", n_free_out, 1, dev), _ints("copies", copies, 2 * forks, dev), _ints("n_copies", n_copies, 1, dev),
-                             _stream_of(lens)))
+    _launch(dev, lib.vf_pages_fork, C.byref(a), forks, _ints("src", src, forks, dev), _ints("dst", dst, forks, dev), _ints("tokens", tokens, forks, dev),
+            _ints("lens", lens, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev),
+            block_table.data_ptr(), _ints("shares", shares, 1, dev), _ints("kv_len", kv_len, a.n_seqs, dev),
+            _ints("n_free_out", n_free_out, 1, dev), _ints("copies", copies, 2 * forks, dev), _ints("n_copies", n_copies, 1, dev),
+            _stream_of(lens))
 
 
 def vf_pages_keep(lens, keep, free_pages, n_free, block_table, shares, kv_len, n_free_out, copies, n_copies):
@@ -630,10 +643,10 @@ def vf_pages_keep(lens, keep, free_pages, n_free, block_table, shares, kv_len, n
     in place; results kv_len [n], n_free_out [1], copies [n, 2], n_copies [1]."""
     dev = _device("lens", lens)
     a = _pages_args(block_table, shares, free_pages.numel(), dev)
-    _check(lib.vf_pages_keep(C.byref(a), _ints("lens", lens, a.n_seqs, dev), _ints("keep", keep, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev),
-                             _ints("n_free", n_free, 1, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
-                             _ints("kv_len", kv_len, a.n_seqs, dev), _ints("n_free_out", n_free_out, 1, dev),
-                             _ints("copies", copies, 2 * a.n_seqs, dev), _ints("n_copies", n_copies, 1, dev), _stream_of(lens)))
+    _launch(dev, lib.vf_pages_keep, C.byref(a), _ints("lens", lens, a.n_seqs, dev), _ints("keep", keep, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev),
+            _ints("n_free", n_free, 1, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
+            _ints("kv_len", kv_len, a.n_seqs, dev), _ints("n_free_out", n_free_out, 1, dev),
+            _ints("copies", copies, 2 * a.n_seqs, dev), _ints("n_copies", n_copies, 1, dev), _stream_of(lens))
 
 
 def vf_pages_compact(lens, block_table, shares, table_out, shares_out, free_out, n_free_out, moved, copies, n_copies):
@@ -644,10 +657,10 @@ def vf_pages_compact(lens, block_table, shares, table_out, shares_out, free_out,
     n, m, stride = _table(table_out, dev)
     if (n, m) != (a.n_seqs, a.max_pages):
         _refuse(f"table_out: int32 tensor [{a.n_seqs}, {a.max_pages}]{_on(dev)}")
-    _check(lib.vf_pages_compact(C.byref(a), room, stride, _ints("lens", lens, a.n_seqs, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
-                                table_out.data_ptr(), _ints("shares_out", shares_out, 1, dev), _ints("free_out", free_out, room, dev),
-                                _ints("n_free_out", n_free_out, 1, dev), _ints("moved", moved, a.pool_pages, dev),
-                                _ints("copies", copies, 2 * min(a.pool_pages, room), dev), _ints("n_copies", n_copies, 1, dev), _stream_of(lens)))
+    _launch(dev, lib.vf_pages_compact, C.byref(a), room, stride, _ints("lens", lens, a.n_seqs, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
+            table_out.data_ptr(), _ints("shares_out", shares_out, 1, dev), _ints("free_out", free_out, room, dev),
+            _ints("n_free_out", n_free_out, 1, dev), _ints("moved", moved, a.pool_pages, dev),
+            _ints("copies", copies, 2 * min(a.pool_pages, room), dev), _ints("n_copies", n_copies, 1, dev), _stream_of(lens))
 
 
 def _layers(name, t, dev):
@@ -671,8 +684,8 @@ def vf_pages_copy(pools, copies, n_copies, to):
     if to_layers != layers or to_size != size or to.dtype is not pools.dtype:
         _refuse("pools of other layers, heads or types")
     a = vf_copy_args(layers, size, pages, to_pages, copies.numel() // 2, 0, stride, to_stride)
-    _check(lib.vf_pages_copy(C.byref(a), pools.data_ptr(), to.data_ptr(), _ints("copies", copies, 0, dev), _ints("n_copies", n_copies, 1, dev),
-                             _stream_of(pools)))
+    _launch(dev, lib.vf_pages_copy, C.byref(a), pools.data_ptr(), to.data_ptr(), _ints("copies", copies, 0, dev), _ints("n_copies", n_copies, 1, dev),
+            _stream_of(pools))
 
 
 # ---- logits ----------------------------------------------------------------------------------------
@@ -719,8 +732,8 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
             _refuse(f"biases: contiguous float32 tensor of {entries} entries{_on(dev)}")
         bias_off, bias_id, bias = _ints("bias_off", bias_off, n + 1, dev), _ints("bias_id", bias_id, 0, dev), bias.data_ptr()
     a = vf_logits_args(_dtype(logits), n, rows, vocab, text_most, entries, masks, 0, in_stride, out_stride, text_stride, mask_stride)
-    _check(lib.vf_logits_adjust(C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), penalty, text,
-                                None if history_len is None else _ints("history_len", history_len, n, dev),
-                                None if prompt_len is None else _ints("prompt_len", prompt_len, n, dev),
-                                None if tokens is None else _ints("tokens", tokens, rows, dev), bias_off, bias_id, bias, bits,
-                                None if mask_row is None else _ints("mask_row", mask_row, rows, dev), _stream_of(logits)))
+    _launch(dev, lib.vf_logits_adjust, C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), penalty, text,
+            None if history_len is None else _ints("history_len", history_len, n, dev),
+            None if prompt_len is None else _ints("prompt_len", prompt_len, n, dev),
+            None if tokens is None else _ints("tokens", tokens, rows, dev), bias_off, bias_id, bias, bits,
+            None if mask_row is None else _ints("mask_row", mask_row, rows, dev), _stream_of(logits))

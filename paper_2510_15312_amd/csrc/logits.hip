@@ -114,6 +114,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
         if (r >= end) {        // the first row, or the first of another sequence
             int id[TEXT], n = 0, prompt = 0, first = 0, b0 = 0, b1 = 0;
             __amdgpu_buffer_rsrc_t text;
+            if (r > r0) seq = min(seq + 1, a.n_seqs - 1);
             for (bool sure = false;; sure = true) {
                 // all that depends on the sequence alone is asked for with its offsets
                 text = piece(x.history + (size_t)seq * a.history_stride, a.max_history * 4);

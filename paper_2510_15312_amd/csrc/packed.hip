@@ -178,17 +178,20 @@ __device__ __forceinline__ void turn_unit(float *x, const float2 *angle, bool ha
 // over BATCH heads and asks for all their pieces before it turns the first.
 // 8192 rows of 24 + 2 x 8 heads of 128: 39.3 us = 4.4 TB/s where a large copy reaches 4.8; 16 rows at 1.5B 3.1 us, the launch and
 // three dependent reads (position, angles, elements).
-constexpr int ROTARY_ROWS = 16, ROTARY_V_ROWS = 64, BATCH = 4;
+constexpr int ROTARY_ROWS = 16, ROTARY_V_ROWS = 64;
 
 struct RotaryGrid { int32_t heads, v, k, v_rows, v_single; };   // heads a workgroup of q or k; workgroups of v, of k; rows a workgroup of v; each by itself
 
-struct HeadNorms { vf_head_norm n; };                      // norms of q and k before they turn
-struct NoNorms {};
+// Norms of q and k before they turn: a sum of squares over a head, which lies in neighbouring lanes of a wavefront, and a gain for each element.
+// That takes registers, so BATCH is 2 with them (8192 rows of 24 + 2 x 8 heads of 128: 41.7 us with four heads at a time, 38.8 with two, 47.4 with
+// eight) and 4 without.
+struct HeadNorms { static constexpr int BATCH = 2; vf_head_norm n; };
+struct NoNorms { static constexpr int BATCH = 4; };
 
 template <typename T, int HD, bool HALF, typename NORM>
 __device__ __forceinline__ void rotate_rows(const vf_rotary_args &a, const NORM &norm, const T *src, int64_t src_stride, const float2 *table,
                                             const int32_t *pos, const int32_t *slot, T *out, bool is_k, int row, int ui, int h, int h1) {
-    constexpr int SIDE = 256 / (ROTARY_ROWS * (HD / 16));   // heads side by side
+    constexpr int SIDE = 256 / (ROTARY_ROWS * (HD / 16)), BATCH = NORM::BATCH;   // heads side by side, heads a thread at a time
     constexpr bool NORMED = std::is_same<NORM, HeadNorms>::value;
     if (row >= a.total_rows) return;
     const Unit u = unit_of(ui, a.rotary_dim, HALF);
@@ -365,8 +368,8 @@ int launch_rotary(const char *name, const vf_rotary_args &a, const NORM &norm, c
                   const int32_t *slot, void *q_out, void *kv, hipStream_t st) {
     const int tiles = (a.total_rows + ROTARY_ROWS - 1) / ROTARY_ROWS, side = 256 / (ROTARY_ROWS * (HD / 16));
     RotaryGrid g;
-    // as many heads a workgroup as leave the chip about eight workgroups a compute unit, at most BATCH for a thread
-    g.heads = std::min((int)std::max(1ll, (long long)tiles * (a.n_q_heads + a.n_kv_heads) / (2048 * side)), BATCH) * side;
+    // as many heads a workgroup as leave the chip about eight workgroups a compute unit, at most a batch for a thread
+    g.heads = std::min((int)std::max(1ll, (long long)tiles * (a.n_q_heads + a.n_kv_heads) / (2048 * side)), NORM::BATCH) * side;
     // v: up to 128 K elements each row by itself (777 rows of two heads of 64: 3.0 us a call for 3.4), else tiles of 64 rows, or of
     // 32 or 16 where that leaves fewer than 100 workgroups (512 rows of eight heads of 128: 5.7, 5.1, 4.8; 2000 of two: 7.2, 6.4, 6.7)
     g.v_single = (long long)a.total_rows * a.n_kv_heads * HD <= 128 * 1024;

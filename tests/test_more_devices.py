@@ -4,12 +4,32 @@ import pytest
 import torch
 
 import paper_2510_15312_amd as vf
+from paper_2510_15312_amd import binding
 from test_packed_devices import BF16, F32, I32, ROTARY, On, reached  # noqa: F401
 
 
 class Sized(On):
     def element_size(self):
         return {BF16: 2, F32: 4, I32: 4}[self.dtype]
+
+
+@pytest.fixture
+def current(monkeypatch):
+    """The current device is 1; the devices that were made current for a call."""
+    made = []
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+
+    class Device:
+        def __init__(self, number):
+            self.number = number
+
+        def __enter__(self):
+            made.append(self.number)
+
+        def __exit__(self, *args):
+            pass
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    return made
 
 
 NORM = dict(ROTARY, q_gain=(F32, 64), k_gain=(F32, 2, 64))
@@ -32,9 +52,15 @@ def _tensors(tensors, device, other=None, there=None):
 
 
 @pytest.mark.parametrize("call,tensors,more", CALLS)
-def test_one_device(reached, call, tensors, more):  # noqa: F811
+def test_one_device(reached, current, call, tensors, more):  # noqa: F811
     call(**_tensors(tensors, 1), **more)
-    assert reached == [call.__name__]
+    assert reached == [call.__name__] and not current
+
+
+@pytest.mark.parametrize("call,tensors,more", CALLS)
+def test_a_device_that_is_not_the_current_one(reached, current, call, tensors, more):  # noqa: F811
+    call(**_tensors(tensors, 2), **more)
+    assert reached == [call.__name__] and current == [2]
 
 
 @pytest.mark.parametrize("call,tensors,more,other", [(c, t, m, name) for c, t, m in CALLS for name in t])
@@ -46,7 +72,7 @@ def test_a_tensor_of_another_device(reached, call, tensors, more, other, device)
 
 
 @pytest.mark.parametrize("other", [None, 0, 1, 2])
-def test_biases(reached, other):  # noqa: F811
+def test_biases(reached, current, other):  # noqa: F811
     biases = tuple(Sized(0 if i == other else 1, *spec) for i, spec in enumerate(BIASES))
     if other is None:
         vf.vf_logits_adjust(**_tensors(LOGITS, 1), biases=biases)
@@ -76,7 +102,7 @@ def test_other_types_and_shapes(reached, which, other, spec):  # noqa: F811
     assert not reached
 
 
-def test_fewer_masks_than_rows(reached):  # noqa: F811
+def test_fewer_masks_than_rows(reached, current):  # noqa: F811
     args = _tensors(dict(LOGITS, mask=(I32, 4, 4)), 1)
     vf.vf_logits_adjust(**args)
     with pytest.raises(vf.VfError):

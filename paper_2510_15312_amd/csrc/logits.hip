@@ -47,9 +47,11 @@ template <typename T, int N> __device__ __forceinline__ Some<T, N> read_some(__a
     else if constexpr (BYTES == 4) return __builtin_bit_cast(Some<T, N>, __builtin_amdgcn_raw_buffer_load_b32(p, at, 0, 0));
     else return __builtin_bit_cast(Some<T, N>, __builtin_amdgcn_raw_buffer_load_b16(p, at, 0, 0));
 }
-template <int N> __device__ __forceinline__ void write_some(__amdgpu_buffer_rsrc_t p, int element, const Some<float, N> &x) {
-    if constexpr (N == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, x), p, element * 4, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), p, element * 4, 0, 0);
+// PAST: not kept in the caches
+template <int N, bool PAST> __device__ __forceinline__ void write_some(__amdgpu_buffer_rsrc_t p, int element, const Some<float, N> &x) {
+    constexpr int NT = PAST ? 2 : 0;
+    if constexpr (N == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, x), p, element * 4, 0, NT);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), p, element * 4, 0, NT);
 }
 
 struct Penalty { float repetition, inverse, presence, frequency; };
@@ -73,7 +75,7 @@ __device__ __forceinline__ float penalised(float z, unsigned count, const Penalt
 // biases each take 20.4 us in a graph, 13.7 without the tables, 17.7 without text; seven workgroups a compute unit hide the rest of it.
 // One row of 151,936 ids 4.3 us, 270 rows of 16 sequences with everything 84 us (3.97 TB/s; a large copy 4.74).
 // Rows that do not start at a multiple of four ids keep fewer tokens in flight, for eight wavefronts a SIMD: 100 rows of 100,003 ids 24.4 us for 26.5.
-template <typename T, int SLICE, bool VEC>
+template <typename T, int SLICE, bool VEC, bool PAST>
 __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kernel(vf_logits_args a, LogitsArrays x, const T *logits, float *out, int slices,
                                                                       int rows_each) {
     constexpr int EACH = SLICE / LOGIT_THREADS, STEP = VEC ? 4 : 1, TEXT = VEC ? 8 : 4, BIASES = 2;   // ids a thread, how many side by side, tokens and
@@ -231,31 +233,40 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 }
 #pragma unroll
                 for (int j = 0; j < STEP; ++j) y.v[j] = bits[i] >> j & 1 ? y.v[j] : -INFINITY;
-                if (touched) write_some<STEP>(to, id_of(i), y);
+                if (touched) write_some<STEP, PAST>(to, id_of(i), y);
             }
         }
     }
 }
 
-template <typename T, int SLICE, bool VEC>
-int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
+template <typename T, int SLICE, bool VEC, bool PAST>
+int launch_slices(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
     const int slices = (a.vocab + SLICE - 1) / SLICE;
     // rows that are likely to be of one sequence share its tables, up to four and as long as about 1500 workgroups are left (136 rows of 8
     // sequences, 151,936 ids: one row each 45.4 us, two 40.5, three 39.4, four 40.9, nine 41.5)
     const long long all = (long long)slices * a.total_rows, fit = std::min({4ll, (long long)a.total_rows / a.n_seqs, all / 1500});
     const int rows_each = (int)std::max({1ll, fit, all / 0x7fffff});    // (a launch takes 2^24 workgroups)
     const long long blocks = (long long)slices * ((a.total_rows + rows_each - 1) / rows_each);
-    hipLaunchKernelGGL((logits_adjust_kernel<T, SLICE, VEC>), dim3((unsigned)blocks), dim3(LOGIT_THREADS), 0, st, a, x, (const T *)logits, out, slices,
+    hipLaunchKernelGGL((logits_adjust_kernel<T, SLICE, VEC, PAST>), dim3((unsigned)blocks), dim3(LOGIT_THREADS), 0, st, a, x, (const T *)logits, out, slices,
                        rows_each);
     VF_LAUNCH_CHECK("logits_adjust");
     return VF_OK;
+}
+
+// Results of 100 MB and more go past the caches, which do not hold them until they are read: 200 rows of 151,936 ids and a kernel that reads
+// them behind it 99 us for 107; 150 rows (91 MB) would be written faster too (40.6 for 44.9), but read
+// slower by more (together 87 for 82).
+template <typename T, int SLICE, bool VEC>
+int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
+    return 4ll * a.total_rows * a.vocab >= 100'000'000 ? launch_slices<T, SLICE, VEC, true>(a, x, logits, out, st)
+                                                       : launch_slices<T, SLICE, VEC, false>(a, x, logits, out, st);
 }
 
 // Ids a workgroup: the text is read once for each slice of a row, so larger slices read it less often and leave fewer workgroups.
 template <typename T, bool VEC> int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
     const long long thousands = (a.vocab + 1023ll) / 1024 * a.total_rows;
     // few of them: one row of 151,936 ids 4.3 us for 4.7, four 5.5 for 5.9, eight 7.2 for 6.4
-    if (thousands <= 800) return launch<T, 1024, VEC>(a, x, logits, out, st);
+    if (thousands <= 800) return launch_slices<T, 1024, VEC, false>(a, x, logits, out, st);
     // many rows of a sequence each with long texts (200 rows, texts of 2000: 56.5 us for 60.6, of 8000: 69.5 for 77.0; of 200: 57.5 for 54.5)
     if (VEC && thousands > 16384 && a.max_history >= 1024 && a.total_rows < 2ll * a.n_seqs) return launch<T, VEC ? 4096 : 2048, VEC>(a, x, logits, out, st);
     return launch<T, 2048, VEC>(a, x, logits, out, st);

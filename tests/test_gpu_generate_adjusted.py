@@ -6,7 +6,10 @@ import oracle
 from oracle import packed as op
 import workloads as wl
 from paper_2510_15312_amd.generate import generate
-from util_gpu import Pair
+import torch
+
+import paper_2510_15312_amd as vf
+from util_gpu import DEV, Pair, f32, gpu_accept, i32, accept_margin_ok
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +73,46 @@ def test_ids_outside_the_vocabulary_are_refused():
     pair = Pair(cfg, max_rows=128, max_positions=600)
     with pytest.raises(ValueError):
         generate(pair.model, pair.new_seq(600), _prompt(cfg), 3, chunk=64, allowed=lambda text: [cfg.vocab])
+
+
+@pytest.mark.parametrize("mode", ["greedy", "stochastic"])
+def test_verify_adjust_accept(mode):
+    """The three calls of a step, with masks and penalties: accepted and emitted tokens are what the oracle's rule makes of the
+    adjusted logits, and of the allowed ids."""
+    cfg = wl.CONFIGS["tiny_f32"]
+    pair, prompt, rng = Pair(cfg, max_rows=128, max_positions=600), _prompt(cfg), np.random.default_rng(8)
+    seen = 0
+    for step in range(6):
+        seq = pair.new_seq(600)
+        vf.vf_prefill_chunk(pair.model, seq, i32(prompt[:100]))
+        vf.vf_prefill_chunk(pair.model, seq, i32(prompt[100:]), sample_first=True)
+        _, pending = vf.vf_seq_get_state(seq)
+        k = 5
+        allowed = rng.random((k + 1, cfg.vocab)) < 0.03
+        drafts = [int(rng.choice(np.flatnonzero(allowed[i]))) for i in range(k)]
+        tokens, logits = i32([pending] + drafts), torch.empty((k + 1, cfg.vocab), device=DEV)
+        vf.vf_verify(pair.model, [seq], tokens, [0, k + 1], logits)
+        before = logits.double().cpu().numpy()
+        words = torch.as_tensor(np.packbits(allowed, axis=1, bitorder="little").view(np.int32), device=DEV)
+        vf.vf_logits_adjust(logits, i32([0, k + 1]), logits, f32([[1.2, 0.3, 0.1]]), i32([prompt]), i32([len(prompt)]), i32([len(prompt)]), tokens, mask=words)
+        z = logits.cpu().numpy()
+        want = op.logits_adjust(before, [0, k + 1], [(np.float32(1.2), np.float32(0.3), np.float32(0.1))], [prompt], [len(prompt)], [pending] + drafts, mask=allowed)
+        assert np.array_equal(np.isneginf(z), ~allowed) and np.allclose(z[allowed], want[allowed], rtol=2.0 ** -21, atol=2.0 ** -21)
+        if step % 2:                                                 # drafts that are accepted for a while
+            tokens = i32([pending] + [int(v) for v in z[:k].argmax(1)])
+            drafts = tokens.tolist()[1:]
+        u = rng.random(2 * (k + 1)).astype(np.float32)
+        temperature = 0.7
+        params = [(vf.VF_GREEDY, 0.0, None, None)] if mode == "greedy" else [(vf.VF_STOCHASTIC, temperature, None, f32(u))]
+        n_acc, out, y = gpu_accept(pair, [seq], tokens, [0, k + 1], params, logits)
+        a = int(n_acc[0])
+        assert allowed[a, out[a]] and all(allowed[i, out[i]] for i in range(a))
+        if mode == "greedy":
+            want_a, want_out, _ = oracle.greedy_accept(z, drafts)
+        else:
+            if not accept_margin_ok(z, drafts, mode, None, u, temperature, 1e-9):
+                continue
+            want_a, want_out, _ = oracle.stochastic_accept(z, drafts, None, u, temperature)
+        assert a == want_a and np.array_equal(out[:a + 1], want_out) and np.array_equal(y, z.argmax(1))
+        seen += 1
+    assert seen >= 4

@@ -141,6 +141,34 @@ def test_many_rows_a_workgroup():
     Call(23, 66000, [40, 1, 300], most=9000).run()
 
 
+@pytest.mark.parametrize("vocab", [70000, 70001])
+def test_results_that_the_caches_do_not_hold(vocab):
+    c = Call(53, vocab, [1] * 200 + [0, 33, 150], most=2500)
+    c.run()
+    c.run(in_place=True)
+
+
+@pytest.mark.parametrize("vocab,entries", [(4096, 700), (700, 5000), (151936, 3000)])
+def test_long_lists_of_biases(vocab, entries):
+    """More biases than a workgroup holds at a time, ids several times among them and outside the vocabulary."""
+    c, rng = Call(43, vocab, [2, 1, 5], what="penalties history tokens biases"), np.random.default_rng(4)
+    c.kw["biases"] = [[(int(v), float(np.float32(x))) for v, x in zip(rng.integers(-5, vocab // 2 + 9, m), rng.normal(size=m))] for m in (entries, 0, entries // 3)]
+    c.run()
+
+
+def test_a_bias_of_the_values_that_numbers_of_places_have():
+    """Places in the list are told from values: a value with the bits of a small whole number, zeros of both signs, one id many times."""
+    vocab = 1500
+    values = np.arange(1, 600, dtype=np.int32).view(np.float32)            # denormal numbers
+    biases = (i32([0, 599, 602]), i32([7] * 599 + [3, 3, 4]), f32(np.concatenate([values, np.float32([5.0, 0.0, -0.0])])))
+    z = torch.zeros((2, vocab), device=DEV)
+    out = torch.full_like(z, 9.0)
+    vf.vf_logits_adjust(z, i32([0, 1, 2]), out, biases=biases)
+    want = np.zeros((2, vocab), np.float32)
+    want[0, 7] = values[-1]
+    assert np.array_equal(out.cpu().numpy(), want)
+
+
 def test_no_rows_and_rows_outside():
     Call(29, 100, [0, 0]).run()
     c = Call(31, 5000, [3, 4, 2])

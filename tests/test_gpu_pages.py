@@ -196,6 +196,29 @@ def test_many_entries_at_once():
     same(fork(*args), op.pages_fork(*args))
 
 
+def test_a_large_pool():
+    """More pages than a word of bits for every thread."""
+    rng, pool = np.random.default_rng(9), 200_003
+    n, width = 300, 500
+    lens = rng.integers(0, 64 * width, n)
+    held = -(-lens // 64)
+    ids = rng.permutation(pool)[:held.sum()]
+    table, at = np.full((n, width), -1), 0
+    for b in range(n):
+        table[b, :held[b]] = ids[at:at + held[b]]
+        at += held[b]
+    table[7, :held[7]][:20], shares = table[8, :held[8]][:20], np.zeros(pool, int)
+    shares[table[8, :20]] = 1
+    for room in (pool, int(held.sum()) - 30):
+        same(compact(lens, table, shares, room), op.pages_compact(lens, table, shares, room))
+    free = np.full(pool, -1)
+    kept = rng.integers(0, 64 * width, n)
+    args = lens, kept, free, 0, table, shares
+    same(keep(*args), op.pages_keep(*args))
+    with pytest.raises(vf.VfError):
+        compact(lens, table, np.zeros(vf.VF_PAGES_MAX_POOL + 1, int), 5)
+
+
 def test_table_rows_apart():
     wide = torch.full((4, 9), JUNK, dtype=torch.int32, device=DEV)
     table = wide[:, 2:5]
@@ -237,6 +260,20 @@ def test_copies(n, layers, hkv, hd, dtype):
     if n:
         want[0, pairs[:, 1]] = pools[0, pairs[:, 0]]
     assert torch.equal(other, want)
+
+
+@pytest.mark.parametrize("shape", [(2, 1, 24), (2, 3, 4104), (2, 1, 2048), (2, 5, 4100)])
+def test_pages_of_other_sizes(shape):
+    """Pages that are no multiple of what a workgroup moves at a time; a view of some layers of a wider pool."""
+    pools = torch.randn((4, 11, *shape), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    want = pools.clone()
+    want[1:3, [0, 10]] = pools[1:3, [5, 3]]
+    vf.vf_pages_copy(pools[1:3], i32([[5, 0], [3, 10]]), i32([2]), pools[1:3])
+    assert torch.equal(pools, want)
+    with pytest.raises(vf.VfError):
+        vf.vf_pages_copy(pools.transpose(0, 1), i32([[3, 0]]), i32([1]), pools.transpose(0, 1))
+    with pytest.raises(vf.VfError):
+        vf.vf_pages_copy(pools[..., :-1], i32([[5, 0]]), i32([1]), pools[..., :-1])
 
 
 def test_copies_that_are_left_out():

@@ -114,25 +114,24 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
             }
         }
         if (r >= end) {        // the first row, or the first of another sequence
-            int id[TEXT], n = 0, prompt = 0, first = 0, b0 = 0, b1 = 0;
+            int id[TEXT], first, length, prompt, b0, b1;
             __amdgpu_buffer_rsrc_t text;
             if (r > r0) seq = min(seq + 1, a.n_seqs - 1);
             for (bool sure = false;; sure = true) {
-                // all that depends on the sequence alone is asked for with its offsets
-                text = piece(x.history + (size_t)seq * a.history_stride, a.max_history * 4);
-                if (x.history) {
+                // All that depends on the sequence alone is asked for with its offsets, without conditions, whose ends would wait for it: what is
+                // not there is read from the offsets instead, and not used.
+                text = piece(x.history ? x.history + (size_t)seq * a.history_stride : x.row_off, x.history ? a.max_history * 4 : 0);
 #pragma unroll
-                    for (int j = 0; j < TEXT; ++j) id[j] = read_some<int, 1>(text, tid + j * LOGIT_THREADS).v[0];
-                    n = min(max(x.history_len[seq], 0), a.max_history);
-                    prompt = x.prompt_len ? min(max(x.prompt_len[seq], 0), n) : 0;
-                }
-                if (x.penalties) p = Penalty{x.penalties[3 * seq], 0.f, x.penalties[3 * seq + 1], x.penalties[3 * seq + 2]};
-                if (x.bias_off) {
-                    b0 = max(x.bias_off[seq], 0);
-                    b1 = min(x.bias_off[seq + 1], a.bias_entries);
-                }
+                for (int j = 0; j < TEXT; ++j) id[j] = read_some<int, 1>(text, tid + j * LOGIT_THREADS).v[0];
+                const float *penalties = x.penalties ? x.penalties + 3 * (size_t)seq : reinterpret_cast<const float *>(x.row_off);
+                const int32_t *biases = x.bias_off ? x.bias_off + seq : x.row_off;
                 first = x.row_off[seq];
                 end = x.row_off[seq + 1];
+                p = Penalty{penalties[0], 0.f, penalties[1], penalties[x.penalties ? 2 : 1]};
+                length = (x.history ? x.history_len : x.row_off)[seq];
+                prompt = (x.prompt_len ? x.prompt_len : x.row_off)[seq];
+                b0 = biases[0];
+                b1 = biases[1];
                 inside = first >= 0 && first <= r && r < end;
                 if (sure || inside) break;
                 seq = sequence_of(x.row_off, a.n_seqs, r);
@@ -145,8 +144,12 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
             end = max(end, r + 1);
             if (inside) {
                 counted = x.penalties && (p.repetition != 1.f || p.presence != 0.f || p.frequency != 0.f);
-                biased = b0 < b1;
                 p.inverse = 1.f / p.repetition;
+                const int n = x.history ? min(max(length, 0), a.max_history) : 0;
+                prompt = x.prompt_len ? min(max(prompt, 0), n) : 0;
+                b0 = max(b0, 0);
+                b1 = x.bias_off ? min(b1, a.bias_entries) : 0;
+                biased = b0 < b1;
                 unsigned bias_id[BIASES];
 #pragma unroll
                 for (int j = 0; j < BIASES; ++j) bias_id[j] = b0 + tid + j * LOGIT_THREADS < b1 ? x.bias_id[b0 + tid + j * LOGIT_THREADS] : -1;

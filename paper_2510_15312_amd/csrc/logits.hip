@@ -1,5 +1,6 @@
 // Penalties for repeated tokens, biases and grammar masks on the logits of packed rows.
 #include <algorithm>
+#include <type_traits>
 
 #include "vf_internal.h"
 
@@ -47,9 +48,10 @@ template <typename T, int N> __device__ __forceinline__ Some<T, N> read_some(__a
     else if constexpr (BYTES == 4) return __builtin_bit_cast(Some<T, N>, __builtin_amdgcn_raw_buffer_load_b32(p, at, 0, 0));
     else return __builtin_bit_cast(Some<T, N>, __builtin_amdgcn_raw_buffer_load_b16(p, at, 0, 0));
 }
-// PAST: not kept in the caches
-template <int N, bool PAST> __device__ __forceinline__ void write_some(__amdgpu_buffer_rsrc_t p, int element, const Some<float, N> &x) {
-    constexpr int NT = PAST ? 2 : 0;
+// How a call writes: through the caches, past them, or over the logits themselves, where only what changes is read and written.
+enum Way { CACHED, PAST, IN_PLACE };
+template <int N, Way WAY> __device__ __forceinline__ void write_some(__amdgpu_buffer_rsrc_t p, int element, const Some<float, N> &x) {
+    constexpr int NT = WAY == PAST ? 2 : 0;
     if constexpr (N == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, x), p, element * 4, 0, NT);
     else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), p, element * 4, 0, NT);
 }
@@ -75,7 +77,7 @@ __device__ __forceinline__ float penalised(float z, unsigned count, const Penalt
 // biases each take 20.4 us in a graph, 13.7 without the tables, 17.7 without text; seven workgroups a compute unit hide the rest of it.
 // One row of 151,936 ids 4.3 us, 270 rows of 16 sequences with everything 84 us (3.97 TB/s; a large copy 4.74).
 // Rows that do not start at a multiple of four ids keep fewer tokens in flight, for eight wavefronts a SIMD: 100 rows of 100,003 ids 24.4 us for 26.5.
-template <typename T, int SLICE, bool VEC, bool PAST>
+template <typename T, int SLICE, bool VEC, Way WAY>
 __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kernel(vf_logits_args a, LogitsArrays x, const T *logits, float *out, int slices,
                                                                       int rows_each) {
     constexpr int EACH = SLICE / LOGIT_THREADS, STEP = VEC ? 4 : 1, TEXT = VEC ? 8 : 4, BIASES = 2;   // ids a thread, how many side by side, tokens and
@@ -84,7 +86,6 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
     __shared__ __align__(16) float bias[SLICE];
     const int tid = threadIdx.x, chunk = blockIdx.x / slices, v0 = (blockIdx.x - chunk * slices) * SLICE;
     const int r0 = chunk * rows_each, r1 = (int)min((long long)r0 + rows_each, (long long)a.total_rows);
-    const bool in_place = (const void *)logits == (const void *)out;
     const int ids = min(SLICE, a.vocab - v0);
     // a thread's ids: four in a row EACH / 4 times, or LOGIT_THREADS apart
     auto id_of = [&](int i) { return i * (STEP * LOGIT_THREADS) + tid * STEP; };
@@ -100,18 +101,19 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
         Some<T, STEP> z[EACH / STEP];
         uint32_t bits[EACH / STEP];
         const auto from = piece(logits + (size_t)r * a.in_stride + v0, ids * (int)sizeof(T));
+        const int m = x.mask ? (x.mask_row ? x.mask_row[r] : r) : -1;
+        const bool masked = m >= 0 && m < a.mask_rows;
+        // over itself, a row without a mask changes in few places, which are read when they are known
+        const bool whole = WAY != IN_PLACE || masked;
+        if (whole)
 #pragma unroll
-        for (int i = 0; i < EACH / STEP; ++i) {
-            z[i] = read_some<T, STEP>(from, id_of(i));
-            bits[i] = 0xffffffffu;
-        }
-        if (x.mask) {
-            const int m = x.mask_row ? x.mask_row[r] : r;
-            if (m >= 0 && m < a.mask_rows) {
-                const auto words = piece(x.mask + (size_t)m * a.mask_stride + v0 / 32, (ids + 31) / 32 * 4);
+            for (int i = 0; i < EACH / STEP; ++i) z[i] = read_some<T, STEP>(from, id_of(i));
 #pragma unroll
-                for (int i = 0; i < EACH / STEP; ++i) bits[i] = read_some<uint32_t, 1>(words, id_of(i) / 32).v[0] >> id_of(i) % 32;
-            }
+        for (int i = 0; i < EACH / STEP; ++i) bits[i] = 0xffffffffu;
+        if (masked) {
+            const auto words = piece(x.mask + (size_t)m * a.mask_stride + v0 / 32, (ids + 31) / 32 * 4);
+#pragma unroll
+            for (int i = 0; i < EACH / STEP; ++i) bits[i] = read_some<uint32_t, 1>(words, id_of(i) / 32).v[0] >> id_of(i) % 32;
         }
         if (r >= end) {        // the first row, or the first of another sequence
             int id[TEXT], first, length, prompt, b0, b1;
@@ -211,19 +213,37 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 }
             }
             const auto to = piece(out + (size_t)r * a.out_stride + v0, ids * 4);
+            constexpr uint32_t ALL = (1u << STEP) - 1;
+            bool touched[EACH / STEP];
+            if constexpr (WAY == IN_PLACE) {
+#pragma unroll
+                for (int i = 0; i < EACH / STEP; ++i) {
+                    unsigned any = 0;
+                    if (counted) {
+                        const Some<unsigned, STEP> c = *reinterpret_cast<const Some<unsigned, STEP> *>(count + id_of(i));
+#pragma unroll
+                        for (int j = 0; j < STEP; ++j) any |= c.v[j];
+                    }
+                    if (biased) {
+                        const Some<unsigned, STEP> b = *reinterpret_cast<const Some<unsigned, STEP> *>(bias + id_of(i));
+#pragma unroll
+                        for (int j = 0; j < STEP; ++j) any |= b.v[j];
+                    }
+                    touched[i] = any || (bits[i] & ALL) != ALL;
+                    if (!whole) z[i] = any ? read_some<T, STEP>(from, id_of(i)) : Some<T, STEP>{};
+                }
+            }
 #pragma unroll
             for (int i = 0; i < EACH / STEP; ++i) {
                 Some<float, STEP> y;
 #pragma unroll
                 for (int j = 0; j < STEP; ++j) y.v[j] = to_f32(z[i].v[j]);
-                bool touched = !in_place || biased || (bits[i] & ((1 << STEP) - 1)) != (1 << STEP) - 1;
                 if (counted) {
                     const Some<unsigned, STEP> c = *reinterpret_cast<const Some<unsigned, STEP> *>(count + id_of(i));
                     unsigned any = 0;
 #pragma unroll
                     for (int j = 0; j < STEP; ++j) any |= c.v[j];
                     if (any) {
-                        touched = true;
 #pragma unroll
                         for (int j = 0; j < STEP; ++j)
                             if (c.v[j]) y.v[j] = penalised(y.v[j], c.v[j], p);
@@ -236,13 +256,13 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 }
 #pragma unroll
                 for (int j = 0; j < STEP; ++j) y.v[j] = bits[i] >> j & 1 ? y.v[j] : -INFINITY;
-                if (touched) write_some<STEP, PAST>(to, id_of(i), y);
+                if (WAY != IN_PLACE || touched[i]) write_some<STEP, WAY>(to, id_of(i), y);
             }
         }
     }
 }
 
-template <typename T, int SLICE, bool VEC, bool PAST>
+template <typename T, int SLICE, bool VEC, Way WAY>
 int launch_slices(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
     const int slices = (a.vocab + SLICE - 1) / SLICE;
     // rows that are likely to be of one sequence share its tables, up to four and as long as about 1500 workgroups are left (136 rows of 8
@@ -250,7 +270,7 @@ int launch_slices(const vf_logits_args &a, const LogitsArrays &x, const void *lo
     const long long all = (long long)slices * a.total_rows, fit = std::min({4ll, (long long)a.total_rows / a.n_seqs, all / 1500});
     const int rows_each = (int)std::max({1ll, fit, all / 0x7fffff});    // (a launch takes 2^24 workgroups)
     const long long blocks = (long long)slices * ((a.total_rows + rows_each - 1) / rows_each);
-    hipLaunchKernelGGL((logits_adjust_kernel<T, SLICE, VEC, PAST>), dim3((unsigned)blocks), dim3(LOGIT_THREADS), 0, st, a, x, (const T *)logits, out, slices,
+    hipLaunchKernelGGL((logits_adjust_kernel<T, SLICE, VEC, WAY>), dim3((unsigned)blocks), dim3(LOGIT_THREADS), 0, st, a, x, (const T *)logits, out, slices,
                        rows_each);
     VF_LAUNCH_CHECK("logits_adjust");
     return VF_OK;
@@ -261,15 +281,17 @@ int launch_slices(const vf_logits_args &a, const LogitsArrays &x, const void *lo
 // slower by more (together 87 for 82).
 template <typename T, int SLICE, bool VEC>
 int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
-    return 4ll * a.total_rows * a.vocab >= 100'000'000 ? launch_slices<T, SLICE, VEC, true>(a, x, logits, out, st)
-                                                       : launch_slices<T, SLICE, VEC, false>(a, x, logits, out, st);
+    if constexpr (std::is_same<T, float>::value)
+        if (logits == out) return launch_slices<T, SLICE, VEC, IN_PLACE>(a, x, logits, out, st);
+    return 4ll * a.total_rows * a.vocab >= 100'000'000 ? launch_slices<T, SLICE, VEC, PAST>(a, x, logits, out, st)
+                                                       : launch_slices<T, SLICE, VEC, CACHED>(a, x, logits, out, st);
 }
 
 // Ids a workgroup: the text is read once for each slice of a row, so larger slices read it less often and leave fewer workgroups.
 template <typename T, bool VEC> int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
     const long long thousands = (a.vocab + 1023ll) / 1024 * a.total_rows;
     // few of them: one row of 151,936 ids 4.3 us for 4.7, four 5.5 for 5.9, eight 7.2 for 6.4
-    if (thousands <= 800) return launch_slices<T, 1024, VEC, false>(a, x, logits, out, st);
+    if (thousands <= 800) return launch<T, 1024, VEC>(a, x, logits, out, st);
     // many rows of a sequence each with long texts (200 rows, texts of 2000: 56.5 us for 60.6, of 8000: 69.5 for 77.0; of 200: 57.5 for 54.5)
     if (VEC && thousands > 16384 && a.max_history >= 1024 && a.total_rows < 2ll * a.n_seqs) return launch<T, VEC ? 4096 : 2048, VEC>(a, x, logits, out, st);
     return launch<T, 2048, VEC>(a, x, logits, out, st);

@@ -500,7 +500,7 @@ int vf_pages_compact(const vf_pages_args *args, int room, int table_out_stride, 
 
 /* Layers of pages of page_bytes each (2 * n_kv_heads * 64 * head_dim elements), layer strides in bytes; max_copies = room of copies. */
 typedef struct {
-    int32_t n_layers, page_bytes, src_pages, dst_pages, max_copies, pad;
+    int32_t n_layers, page_bytes, src_pages, dst_pages, max_copies, pad;   /* page_bytes: a multiple of 16, as strides and addresses */
     int64_t src_layer_stride, dst_layer_stride;
 } vf_copy_args;
 

@@ -513,6 +513,7 @@ int vf_pages_copy(const vf_copy_args *args, const void *src_dev, void *dst_dev, 
 
 #define VF_LOGITS_MAX_VOCAB   (1 << 24)
 #define VF_LOGITS_MAX_HISTORY (1 << 24)
+#define VF_LOGITS_MAX_BIASES  (1 << 28)
 typedef struct {
     int32_t dtype;                  /* of the logits read (VF_F32 | VF_BF16); results are float32 */
     int32_t n_seqs, total_rows, vocab;

@@ -26,7 +26,7 @@ VF_OPT_PERSISTENT = 2
 VF_PACKED_MAX_SEQS, VF_PACKED_MAX_ROWS = 4096, 1 << 20
 VF_ROTARY_HALF, VF_ROTARY_INTERLEAVED = 0, 1
 VF_PAGES_MAX_POOL = 1 << 18
-VF_LOGITS_MAX_VOCAB, VF_LOGITS_MAX_HISTORY = 1 << 24, 1 << 24
+VF_LOGITS_MAX_VOCAB, VF_LOGITS_MAX_HISTORY, VF_LOGITS_MAX_BIASES = 1 << 24, 1 << 24, 1 << 28
 VF_ROTARY_UNSCALED, VF_ROTARY_POSITIONS, VF_ROTARY_BASE, VF_ROTARY_RAMP = 0, 1, 2, 3
 
 EXPORTS = [

@@ -33,6 +33,17 @@ __device__ __forceinline__ int sequence_of(const int32_t *__restrict__ row_off, 
     return not_above - 1;
 }
 
+// A value that is the same for the whole wavefront, through the scalar cache (nobody writes what a call reads): vector loads come back in the
+// order in which they were asked for, so this one does not wait for the logits that are on their way.
+template <typename T> __device__ __forceinline__ T uniform(const T *p, int i) {
+    return reinterpret_cast<const __attribute__((address_space(4))) T *>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
+// Keeps the compiler from putting off such reads to where each is used first, so that they are on their way together.
+__device__ __forceinline__ void together(int a, int b, int c, int d, float e, float f, float g) {
+    asm volatile("" : : "s"(a), "s"(b), "s"(c), "s"(d), "s"(e), "s"(f), "s"(g));
+}
+
 // Loads and stores of a row's piece through a buffer descriptor: one 32-bit offset a lane, and what lies past the piece's end is read as 0
 // and not written, so that no access has a condition of its own.
 typedef unsigned uint4v __attribute__((ext_vector_type(4)));
@@ -82,8 +93,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                                                                       int rows_each) {
     constexpr int EACH = SLICE / LOGIT_THREADS, STEP = VEC ? 4 : 1, TEXT = VEC ? 8 : 4, BIASES = 2;   // ids a thread, how many side by side, tokens and
                                                                                               // biases asked for at a time
-    __shared__ __align__(16) unsigned count[SLICE];
-    __shared__ __align__(16) float bias[SLICE];
+    __shared__ __align__(16) unsigned count[SLICE], bias[SLICE];     // (bias: the bits of a float)
     const int tid = threadIdx.x, chunk = blockIdx.x / slices, v0 = (blockIdx.x - chunk * slices) * SLICE;
     const int r0 = chunk * rows_each, r1 = (int)min((long long)r0 + rows_each, (long long)a.total_rows);
     const int ids = min(SLICE, a.vocab - v0);
@@ -91,7 +101,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
     auto id_of = [&](int i) { return i * (STEP * LOGIT_THREADS) + tid * STEP; };
     for (int i = tid; i < SLICE; i += LOGIT_THREADS) {
         count[i] = 0;
-        bias[i] = 0.f;
+        bias[i] = 0;
     }
     // the tables' sequence, or a guess at the first row's: right where all have as many rows
     int seq = (int)((long long)r0 * a.n_seqs / a.total_rows), end = 0;
@@ -101,7 +111,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
         Some<T, STEP> z[EACH / STEP];
         uint32_t bits[EACH / STEP];
         const auto from = piece(logits + (size_t)r * a.in_stride + v0, ids * (int)sizeof(T));
-        const int m = x.mask ? (x.mask_row ? x.mask_row[r] : r) : -1;
+        const int m = x.mask ? (x.mask_row ? uniform(x.mask_row, r) : r) : -1, own = x.tokens ? uniform(x.tokens, r) : -1;
         const bool masked = m >= 0 && m < a.mask_rows;
         // over itself, a row without a mask changes in few places, which are read when they are known
         const bool whole = WAY != IN_PLACE || masked;
@@ -113,32 +123,29 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
         if (masked) {
             const auto words = piece(x.mask + (size_t)m * a.mask_stride + v0 / 32, (ids + 31) / 32 * 4);
 #pragma unroll
-            for (int i = 0; i < EACH / STEP; ++i) bits[i] = read_some<uint32_t, 1>(words, id_of(i) / 32).v[0] >> id_of(i) % 32;
+            for (int i = 0; i < EACH / STEP; ++i) bits[i] = read_some<uint32_t, 1>(words, id_of(i) / 32).v[0];
         }
         if (r >= end) {        // the first row, or the first of another sequence
-            int id[TEXT], first, length, prompt, b0, b1;
-            __amdgpu_buffer_rsrc_t text;
+            int first, length, prompt, b0, b1;
             if (r > r0) seq = min(seq + 1, a.n_seqs - 1);
             for (bool sure = false;; sure = true) {
-                // All that depends on the sequence alone is asked for with its offsets, without conditions, whose ends would wait for it: what is
-                // not there is read from the offsets instead, and not used.
-                text = piece(x.history ? x.history + (size_t)seq * a.history_stride : x.row_off, x.history ? a.max_history * 4 : 0);
-#pragma unroll
-                for (int j = 0; j < TEXT; ++j) id[j] = read_some<int, 1>(text, tid + j * LOGIT_THREADS).v[0];
+                // all that depends on the sequence alone is asked for with its offsets, without conditions, whose ends would wait for it: what
+                // is not there is read from the offsets instead, and not used
                 const float *penalties = x.penalties ? x.penalties + 3 * (size_t)seq : reinterpret_cast<const float *>(x.row_off);
                 const int32_t *biases = x.bias_off ? x.bias_off + seq : x.row_off;
-                first = x.row_off[seq];
-                end = x.row_off[seq + 1];
-                p = Penalty{penalties[0], 0.f, penalties[1], penalties[x.penalties ? 2 : 1]};
-                length = (x.history ? x.history_len : x.row_off)[seq];
-                prompt = (x.prompt_len ? x.prompt_len : x.row_off)[seq];
-                b0 = biases[0];
-                b1 = biases[1];
+                first = uniform(x.row_off, seq);
+                end = uniform(x.row_off, seq + 1);
+                p = Penalty{uniform(penalties, 0), 0.f, uniform(penalties, 1), uniform(penalties, x.penalties ? 2 : 1)};
+                length = uniform(x.history ? x.history_len : x.row_off, seq);
+                prompt = uniform(x.prompt_len ? x.prompt_len : x.row_off, seq);
+                b0 = uniform(biases, 0);
+                b1 = uniform(biases, 1);
+                together(length, prompt, b0, b1, p.repetition, p.presence, p.frequency);
                 inside = first >= 0 && first <= r && r < end;
                 if (sure || inside) break;
                 seq = sequence_of(x.row_off, a.n_seqs, r);
                 if (seq < 0 || seq >= a.n_seqs) {     // in front of the sequences' rows, or behind them
-                    end = seq < 0 ? x.row_off[0] : a.total_rows;
+                    end = seq < 0 ? uniform(x.row_off, 0) : a.total_rows;
                     seq = max(0, min(seq, a.n_seqs - 1));
                     break;
                 }
@@ -152,6 +159,10 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 b0 = max(b0, 0);
                 b1 = x.bias_off ? min(b1, a.bias_entries) : 0;
                 biased = b0 < b1;
+                const auto text = piece(x.history + (size_t)seq * a.history_stride, n * 4);
+                int id[TEXT];
+#pragma unroll
+                for (int j = 0; j < TEXT; ++j) id[j] = read_some<int, 1>(text, tid + j * LOGIT_THREADS).v[0];
                 unsigned bias_id[BIASES];
 #pragma unroll
                 for (int j = 0; j < BIASES; ++j) bias_id[j] = b0 + tid + j * LOGIT_THREADS < b1 ? x.bias_id[b0 + tid + j * LOGIT_THREADS] : -1;
@@ -159,7 +170,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 if (!clean) {
                     for (int i = tid; i < SLICE; i += LOGIT_THREADS) {
                         count[i] = 0;
-                        bias[i] = 0.f;
+                        bias[i] = 0;
                     }
                     __syncthreads();
                 }
@@ -186,26 +197,29 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                             if (d < SLICE) atomicAdd(&count[d], 2u);
                         }
                 }
-                unsigned *latest = reinterpret_cast<unsigned *>(bias);     // the last bias of an id, numbered from 1 on
-                if (biased) {
+                if (biased) {      // first the number of an id's last bias, from 1 on
 #pragma unroll
                     for (int j = 0; j < BIASES; ++j)
-                        if (bias_id[j] - v0 < SLICE) atomicMax(&latest[bias_id[j] - v0], 1u + tid + j * LOGIT_THREADS);
+                        if (bias_id[j] - v0 < SLICE) atomicMax(&bias[bias_id[j] - v0], 1u + tid + j * LOGIT_THREADS);
                     for (int i = b0 + tid + BIASES * LOGIT_THREADS; i < b1; i += LOGIT_THREADS)
-                        if (const unsigned d = (unsigned)x.bias_id[i] - v0; d < SLICE) atomicMax(&latest[d], 1u + (i - b0));
+                        if (const unsigned d = (unsigned)x.bias_id[i] - v0; d < SLICE) atomicMax(&bias[d], 1u + (i - b0));
                 }
                 if (counted || biased) __syncthreads();
-                if (biased)        // a thread puts the values in the places of its own ids
+                if (biased) {      // a thread puts the values in the places of its own ids; without a number it reads past the list: 0
+                    const auto values = piece(x.bias + b0, (b1 - b0) * 4);
+                    unsigned value[EACH];
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i) {
-                        const int at = id_of(i / STEP) + i % STEP;
-                        if (const unsigned number = latest[at]) bias[at] = x.bias[b0 + (number - 1)];
-                    }
+                    for (int i = 0; i < EACH; ++i) value[i] = bias[id_of(i / STEP) + i % STEP];
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) value[i] = read_some<unsigned, 1>(values, (int)value[i] - 1).v[0];
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) bias[id_of(i / STEP) + i % STEP] = value[i];
+                }
             }
         }
         if (inside) {
             if (counted && x.tokens) {
-                const unsigned d = (unsigned)x.tokens[r] - v0;
+                const unsigned d = (unsigned)own - v0;
                 if (d < SLICE) {
                     __syncthreads();     // the rows before have been read
                     if (tid == 0) count[d] += 2;
@@ -214,6 +228,8 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
             }
             const auto to = piece(out + (size_t)r * a.out_stride + v0, ids * 4);
             constexpr uint32_t ALL = (1u << STEP) - 1;
+#pragma unroll
+            for (int i = 0; i < EACH / STEP; ++i) bits[i] >>= id_of(i) % 32;
             bool touched[EACH / STEP];
             if constexpr (WAY == IN_PLACE) {
 #pragma unroll
@@ -250,9 +266,9 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                     }
                 }
                 if (biased) {
-                    const Some<float, STEP> b = *reinterpret_cast<const Some<float, STEP> *>(bias + id_of(i));
+                    const Some<unsigned, STEP> b = *reinterpret_cast<const Some<unsigned, STEP> *>(bias + id_of(i));
 #pragma unroll
-                    for (int j = 0; j < STEP; ++j) y.v[j] += b.v[j];
+                    for (int j = 0; j < STEP; ++j) y.v[j] += __uint_as_float(b.v[j]);
                 }
 #pragma unroll
                 for (int j = 0; j < STEP; ++j) y.v[j] = bits[i] >> j & 1 ? y.v[j] : -INFINITY;
@@ -326,7 +342,7 @@ extern "C" int vf_logits_adjust(const vf_logits_args *args, const void *logits_d
                        (const void *)history_len_dev);
     if (!history_dev && prompt_len_dev) return vf_fail(VF_ERR_ARG, "vf_logits_adjust: prompt lengths without a history");
     if ((history_dev || tokens_dev) && !penalties_dev) history_dev = tokens_dev = nullptr;    // nothing counts them
-    if (bias_off_dev && (a.bias_entries < 0 || (a.bias_entries > 0 && (!bias_id_dev || !bias_dev))))
+    if (bias_off_dev && (a.bias_entries < 0 || a.bias_entries > VF_LOGITS_MAX_BIASES || (a.bias_entries > 0 && (!bias_id_dev || !bias_dev))))
         return vf_fail(VF_ERR_ARG, "vf_logits_adjust: %d biases", a.bias_entries);
     if (mask_dev && (a.mask_rows < 0 || a.mask_stride < (a.vocab + 31) / 32 || (!mask_row_dev && a.mask_rows < a.total_rows)))
         return vf_fail(VF_ERR_ARG, "vf_logits_adjust: %d masks, stride %lld", a.mask_rows, (long long)a.mask_stride);

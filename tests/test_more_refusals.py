@@ -150,7 +150,7 @@ def _without(*which, n=13):
     (dict(dtype=2), ARG), (dict(n_seqs=0), ARG), (dict(n_seqs=vf.VF_PACKED_MAX_SEQS + 1), ARG), (dict(total_rows=-1), ARG),
     (dict(total_rows=vf.VF_PACKED_MAX_ROWS + 1), ARG), (dict(vocab=0), ARG), (dict(vocab=vf.VF_LOGITS_MAX_VOCAB + 1, in_stride=1 << 30, out_stride=1 << 30), ARG),
     (dict(in_stride=99), ARG), (dict(out_stride=99), ARG), (dict(max_history=-1), ARG), (dict(max_history=vf.VF_LOGITS_MAX_HISTORY + 1, history_stride=1 << 30), ARG),
-    (dict(history_stride=4), ARG), (dict(bias_entries=-1), ARG), (dict(mask_rows=-1), ARG), (dict(mask_stride=3), ARG),
+    (dict(history_stride=4), ARG), (dict(bias_entries=-1), ARG), (dict(bias_entries=vf.VF_LOGITS_MAX_BIASES + 1), ARG), (dict(mask_rows=-1), ARG), (dict(mask_stride=3), ARG),
     (dict(ptrs=_without(0)), ARG), (dict(ptrs=_without(1)), ARG), (dict(ptrs=_without(2)), ARG),
     (dict(ptrs=_without(5)), ARG),                              # a history without lengths
     (dict(ptrs=_without(4)), ARG),                              # prompt lengths without a history

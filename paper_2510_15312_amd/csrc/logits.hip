@@ -82,11 +82,11 @@ __device__ __forceinline__ float penalised(float z, unsigned count, const Penalt
 // once for the rows of a sequence, and a row adds its own token.  Counts are whole numbers, so the order of the additions does not
 // matter, and of several biases of an id the last of the list is found as a maximum over their places.
 //
-// It is bound by memory, and for few rows by reads that wait for one another, so all that depends on the sequence alone is asked for with
-// its offsets, for a sequence that is guessed (right where all have as many rows): then come biases and masks, and the tables.  What
-// the tables cost is time in which a workgroup's loads and stores rest: 70 rows of 128,256 bfloat16 logits with texts of 1500 and 300
-// biases each take 19.8 us in a graph (2.76 TB/s), about 14 without the tables; seven workgroups a compute unit hide the rest of it.
-// One row of 151,936 ids 4.1 us, 270 rows of 16 sequences with everything 75.4 us (4.42 TB/s; a large copy 4.74).
+// It is bound by memory, and for few rows by reads that wait for one another: all that depends on the sequence alone is asked for with its offsets,
+// for a sequence that is guessed (right where all have as many rows), then come the text, biases and masks, and the tables.  What the
+// tables cost is time in which a workgroup's loads and stores rest: 70 rows of 128,256 bfloat16 logits with texts of 1500 and 300 biases each take
+// 17.8 us in a graph (3.07 TB/s), about 13 without the tables; seven workgroups a compute unit hide the rest of it.  One row of
+// 151,936 ids 3.9 us, 270 rows of 16 sequences with everything 66.5 us (5.0 TB/s; a large copy 4.74).
 // Rows that do not start at a multiple of four ids keep fewer tokens in flight, for eight wavefronts a SIMD: 100 rows of 100,003 ids 24.4 us for 26.5.
 template <typename T, int SLICE, bool VEC, Way WAY>
 __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kernel(vf_logits_args a, LogitsArrays x, const T *logits, float *out, int slices,
@@ -281,9 +281,10 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
 template <typename T, int SLICE, bool VEC, Way WAY>
 int launch_slices(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
     const int slices = (a.vocab + SLICE - 1) / SLICE;
-    // rows that are likely to be of one sequence share its tables, up to four and as long as about 1500 workgroups are left (136 rows of 8
-    // sequences, 151,936 ids: one row each 44.0 us, two 39.2, three 37.3, four 39.1, nine 39.6; 170 of 10 with texts of 8000: 61.2, 47.0, 45.3, 43.8, 45.5)
-    const long long all = (long long)slices * a.total_rows, fit = std::min({4ll, (long long)a.total_rows / a.n_seqs, all / 1500});
+    // rows that are likely to be of one sequence share its tables, up to three and as long as about 600 workgroups are left (136 rows of 8
+    // sequences, 151,936 ids: one row each 39.4 us, two 36.3, three 36.5, four 38.1, nine 39.1; 170 of 10 with texts of 8000: 55.8, 44.5, 43.3, 42.6, 43.9;
+    // 17 of one: 9.2, 8.8)
+    const long long all = (long long)slices * a.total_rows, fit = std::min({3ll, (long long)a.total_rows / a.n_seqs, all / 600});
     const int rows_each = (int)std::max({1ll, fit, all / 0x7fffff});    // (a launch takes 2^24 workgroups)
     const long long blocks = (long long)slices * ((a.total_rows + rows_each - 1) / rows_each);
     hipLaunchKernelGGL((logits_adjust_kernel<T, SLICE, VEC, WAY>), dim3((unsigned)blocks), dim3(LOGIT_THREADS), 0, st, a, x, (const T *)logits, out, slices,
@@ -306,9 +307,9 @@ int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, f
 // Ids a workgroup: the text is read once for each slice of a row, so larger slices read it less often and leave fewer workgroups.
 template <typename T, bool VEC> int launch(const vf_logits_args &a, const LogitsArrays &x, const void *logits, float *out, hipStream_t st) {
     const long long thousands = (a.vocab + 1023ll) / 1024 * a.total_rows;
-    // few of them: one row of 151,936 ids 4.3 us for 4.7, four 5.8 for 5.9, eight 7.4 for 6.7
+    // few of them: one row of 151,936 ids 4.1 us for 4.5, four of 100,003 5.8 for 6.7; eight of 151,936 7.4 for 6.6
     if (thousands <= 800) return launch<T, 1024, VEC>(a, x, logits, out, st);
-    // many rows of a sequence each with long texts (200 rows, texts of 2000: 50.8 us for 54.8, of 8000: 62.1 for 69.3; of 200: 50.0 for 49.8)
+    // many rows of a sequence each with room for long texts (200 rows, texts of 8000: 57.7 us for 63.5, of 2000 46.8 for 47.5, of 200 45.8 for 41.3)
     if (VEC && thousands > 16384 && a.max_history >= 1024 && a.total_rows < 2ll * a.n_seqs) return launch<T, VEC ? 4096 : 2048, VEC>(a, x, logits, out, st);
     return launch<T, 2048, VEC>(a, x, logits, out, st);
 }

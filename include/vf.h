@@ -498,7 +498,7 @@ int vf_pages_compact(const vf_pages_args *args, int room, int table_out_stride, 
                      const int32_t *shares_dev, int32_t *table_out_dev, int32_t *shares_out_dev, int32_t *free_out_dev,
                      int32_t *n_free_out_dev, int32_t *moved_dev, int32_t *copies_dev, int32_t *n_copies_dev, void *stream);
 
-/* Layers of pages of page_bytes each (2 * n_kv_heads * 64 * head_dim elements), layer strides in bytes; max_copies = room of copies. */
+/* Layers of pages of page_bytes each (2 * n_kv_heads * 64 * head_dim elements), layer strides in bytes; max_copies = room of copies, at most 2^30. */
 typedef struct {
     int32_t n_layers, page_bytes, src_pages, dst_pages, max_copies, pad;   /* page_bytes: a multiple of 16, as strides and addresses */
     int64_t src_layer_stride, dst_layer_stride;
@@ -531,7 +531,8 @@ typedef struct {
  *   z = -infinity                        where the row's mask has a 0
  * The text of row r is history[b][0 .. history_len[b]), whose first prompt_len[b] tokens are the prompt, and, behind it, the tokens of the
  * sequence's rows up to and with r (tokens[total_rows]: the pending token and the drafts of a verify step, which the history
- * must not have yet).  Ids outside the vocabulary (VF_PENDING too) count nowhere; of several biases of an id the last counts.  Row r has mask
+ * must not have yet).  Ids outside the vocabulary (VF_PENDING too) count nowhere; of several biases of an id the last counts, and offsets of
+ * biases outside 0 .. bias_entries are taken as the nearer of the two.  Row r has mask
  * mask_row[r] (a number outside 0 .. mask_rows - 1: none), id v is bit v % 32 of its word v / 32.  A row whose mask leaves nothing is all
  * -infinity.  penalties is float32 [n_seqs][3], rho > 0.  NULL stands for no penalties, no history, no prompt, no row tokens, no
  * biases, no masks; with mask_row NULL row r has mask r.  Arithmetic is float32.  out may be logits (float32, the same stride).  Rows outside the

@@ -156,8 +156,8 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 p.inverse = 1.f / p.repetition;
                 const int n = x.history ? min(max(length, 0), a.max_history) : 0;
                 prompt = x.prompt_len ? min(max(prompt, 0), n) : 0;
-                b0 = max(b0, 0);
-                b1 = x.bias_off ? min(b1, a.bias_entries) : 0;
+                b1 = x.bias_off ? min(max(b1, 0), a.bias_entries) : 0;
+                b0 = min(max(b0, 0), b1);       // (a sum with an offset far past the list would be negative)
                 biased = b0 < b1;
                 const auto text = piece(x.history + (size_t)seq * a.history_stride, n * 4);
                 int id[TEXT];

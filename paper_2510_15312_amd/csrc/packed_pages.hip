@@ -479,7 +479,8 @@ int vf_pages_copy(const vf_copy_args *args, const void *src_dev, void *dst_dev, 
                   void *stream) {
     if (!args) return vf_fail(VF_ERR_ARG, "vf_pages_copy: NULL argument");
     const vf_copy_args &a = *args;
-    if (a.n_layers < 1 || a.page_bytes < 16 || a.page_bytes > 1 << 30 || a.src_pages < 1 || a.dst_pages < 1 || a.max_copies < 0)
+    if (a.n_layers < 1 || a.page_bytes < 16 || a.page_bytes > 1 << 30 || a.src_pages < 1 || a.dst_pages < 1 || a.max_copies < 0 ||
+        a.max_copies > 1 << 30)
         return vf_fail(VF_ERR_ARG, "vf_pages_copy: %d layers, %d bytes a page, %d and %d pages, %d copies", a.n_layers, a.page_bytes, a.src_pages,
                        a.dst_pages, a.max_copies);
     if (a.n_layers > 1 && (a.src_layer_stride < (int64_t)a.src_pages * a.page_bytes || a.dst_layer_stride < (int64_t)a.dst_pages * a.page_bytes))

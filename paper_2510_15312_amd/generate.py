@@ -21,7 +21,10 @@ class _Adjust:
         self.logits = torch.empty((vf.VF_MAX_DRAFTS + 1, vocab), dtype=torch.float32, device=dev)
         self.more = {}
         if penalties is not None:
-            self.more = dict(penalties=torch.tensor([list(penalties)], dtype=torch.float32, device=dev), prompt_len=ints([len(prompt)]),
+            penalties = list(penalties)
+            if len(penalties) != 3 or not penalties[0] > 0:
+                raise ValueError(f"penalties {penalties}: a repetition above 0, presence, frequency")
+            self.more = dict(penalties=torch.tensor([penalties], dtype=torch.float32, device=dev), prompt_len=ints([len(prompt)]),
                              history=torch.zeros((1, room), dtype=torch.int32, device=dev), history_len=ints([0]))
         if biases:
             self.more["biases"] = (ints([0, len(biases)]), ints(list(biases)), torch.tensor(list(biases.values()), dtype=torch.float32, device=dev))

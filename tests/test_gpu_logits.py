@@ -211,6 +211,19 @@ def test_lengths_outside_the_history():
     assert np.array_equal(out.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("vocab", [300, 301])
+def test_offsets_of_biases_far_outside_the_list(vocab):
+    far, near = (1 << 31) - 1, -(1 << 31)
+    z = torch.ones((4, vocab), device=DEV)
+    for offsets, to in [([far] * 5, [2] * 5), ([near, far, near, far, far], [0, 2, 0, 2, 2]), ([1, far - 1, far, near, 1], [1, 2, 2, 0, 1])]:
+        out, want = torch.empty_like(z), np.ones((4, vocab))
+        for b in range(4):
+            for i in range(to[b], to[b + 1]):
+                want[b, i + 1] = [11.0, 21.0][i]
+        vf.vf_logits_adjust(z, i32([0, 1, 2, 3, 4]), out, biases=(i32(offsets), i32([1, 2]), f32([10.0, 20.0])))
+        assert np.array_equal(out.cpu().numpy(), want), offsets
+
+
 def test_a_row_past_32_bits():
     """Rows that start more than 2^31 elements behind the first."""
     vocab, rows = 151936, 14400

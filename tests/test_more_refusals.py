@@ -5,6 +5,7 @@ import ctypes as C
 import pytest
 
 import paper_2510_15312_amd as vf
+from paper_2510_15312_amd.generate import _Adjust
 
 L, P = vf.lib, C.c_void_p(4096)   # some address
 ARG, UNSUPPORTED, CAP, OK = vf.VF_ERR_ARG, vf.VF_ERR_UNSUPPORTED, vf.VF_ERR_CAP, vf.VF_OK
@@ -123,6 +124,11 @@ def test_copies(kw, code):
     assert _copy(**kw) == code and L.vf_last_error()
 
 
+def test_more_copies_than_indexes_reach():
+    assert _copy(max_copies=(1 << 30) + 1) == ARG and _copy(ptrs=[P, P, None, P], max_copies=1 << 30) == ARG
+    assert b"NULL" in L.vf_last_error()
+
+
 def test_copies_null_and_empty():
     for i in range(4):
         assert _copy(ptrs=[P] * i + [None] + [P] * (3 - i)) == ARG, i
@@ -166,3 +172,9 @@ def test_logits(kw, code):
 def test_logits_null_and_empty():
     assert L.vf_logits_adjust(None, *[P] * 13, None) == ARG
     assert _logits(ptrs=[None] * 13, total_rows=0) == OK
+
+
+@pytest.mark.parametrize("penalties", [(0.0, 0.0, 0.0), (-1.0, 0.1, 0.1), (float("nan"), 0.0, 0.0), (1.0, 0.0), (1.0, 0.0, 0.0, 0.0)])
+def test_penalties_of_generate(penalties):
+    with pytest.raises(ValueError, match="repetition"):
+        _Adjust(penalties, None, None, [1, 2], 10, 20, "cpu")

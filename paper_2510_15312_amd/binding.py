@@ -468,6 +468,12 @@ def _ints(name, t, n, device):
     return t.data_ptr()
 
 
+def _below_31_bits(what, *sizes):
+    """Refuses sizes that the library's 32-bit fields would cut."""
+    if max(sizes) > 0x7fffffff:
+        _refuse(f"{what}: a size of {max(sizes)}")
+
+
 def _rows(name, t, dtype, rows, heads, hd, device):
     """The row stride of a device tensor [rows, heads, hd] whose rows are contiguous."""
     if t.dtype is not dtype or t.shape != (rows, heads, hd) or not t.is_cuda or device is not None and t.get_device() != device:
@@ -622,8 +628,9 @@ def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, ma
 # ---- requests that branch, are cut back or move --------------------------------------------------
 
 def _pages_args(block_table, shares, free_entries, dev):
-    n, m, stride = _table(block_table, dev)
-    return vf_pages_args(n, m, stride, shares.numel(), free_entries, 0)
+    (n, m, stride), pages = _table(block_table, dev), shares.numel()
+    _below_31_bits("pages", stride, pages, free_entries)
+    return vf_pages_args(n, m, stride, pages, free_entries, 0)
 
 
 def vf_pages_fork(src, dst, tokens, lens, free_pages, n_free, block_table, shares, kv_len, n_free_out, copies, n_copies):
@@ -657,6 +664,7 @@ def vf_pages_compact(lens, block_table, shares, table_out, shares_out, free_out,
     n, m, stride = _table(table_out, dev)
     if (n, m) != (a.n_seqs, a.max_pages):
         _refuse(f"table_out: int32 tensor [{a.n_seqs}, {a.max_pages}]{_on(dev)}")
+    _below_31_bits("table_out", stride, room)
     _launch(dev, lib.vf_pages_compact, C.byref(a), room, stride, _ints("lens", lens, a.n_seqs, dev), block_table.data_ptr(), _ints("shares", shares, 1, dev),
             table_out.data_ptr(), _ints("shares_out", shares_out, 1, dev), _ints("free_out", free_out, room, dev),
             _ints("n_free_out", n_free_out, 1, dev), _ints("moved", moved, a.pool_pages, dev),
@@ -683,6 +691,7 @@ def vf_pages_copy(pools, copies, n_copies, to):
     to_layers, to_pages, to_size, to_stride = (layers, pages, size, stride) if to is pools else _layers("to", to, dev)
     if to_layers != layers or to_size != size or to.dtype is not pools.dtype:
         _refuse("pools of other layers, heads or types")
+    _below_31_bits("pools", layers, size, pages, to_pages, copies.numel())
     a = vf_copy_args(layers, size, pages, to_pages, copies.numel() // 2, 0, stride, to_stride)
     _launch(dev, lib.vf_pages_copy, C.byref(a), pools.data_ptr(), to.data_ptr(), _ints("copies", copies, 0, dev), _ints("n_copies", n_copies, 1, dev),
             _stream_of(pools))
@@ -731,6 +740,7 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
                 dev is not None and bias.get_device() != dev:
             _refuse(f"biases: contiguous float32 tensor of {entries} entries{_on(dev)}")
         bias_off, bias_id, bias = _ints("bias_off", bias_off, n + 1, dev), _ints("bias_id", bias_id, 0, dev), bias.data_ptr()
+    _below_31_bits("logits", rows, vocab, text_most, entries, masks)
     a = vf_logits_args(_dtype(logits), n, rows, vocab, text_most, entries, masks, 0, in_stride, out_stride, text_stride, mask_stride)
     _launch(dev, lib.vf_logits_adjust, C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), penalty, text,
             None if history_len is None else _ints("history_len", history_len, n, dev),

@@ -108,3 +108,20 @@ def test_fewer_masks_than_rows(reached, current):  # noqa: F811
     with pytest.raises(vf.VfError):
         vf.vf_logits_adjust(**dict(args, mask_row=None))
     assert reached == ["vf_logits_adjust"]
+
+
+WIDE = 1 << 32      # sizes of which 32 bits would keep what looks right
+TOO_LARGE = [
+    (1, dict(free_pages=(I32, WIDE + 9))), (1, dict(shares=(I32, WIDE + 9))), (2, dict(free_pages=(I32, WIDE + 9))),
+    (3, dict(shares_out=(I32, WIDE + 5), free_out=(I32, WIDE + 5), copies=(I32, 9, 2))),
+    (4, dict(copies=(I32, WIDE, 2))), (4, dict(pools=(BF16, 2, WIDE + 9, 2, 2, 4096))), (4, dict(to=(BF16, 2, WIDE + 5, 2, 2, 4096))),
+    (5, dict(logits=(F32, 5, WIDE + 100), out=(F32, 5, WIDE + 100), mask=(I32, 6, WIDE))), (5, dict(history=(I32, 3, WIDE + 7))),
+    (5, dict(logits=(F32, WIDE + 5, 100), out=(F32, WIDE + 5, 100), tokens=(I32, WIDE + 5), mask_row=(I32, WIDE + 5)))]
+
+
+@pytest.mark.parametrize("which,specs", TOO_LARGE)
+def test_sizes_past_32_bits(reached, current, which, specs):  # noqa: F811
+    call, tensors, more = CALLS[which]
+    with pytest.raises(vf.VfError):
+        call(**_tensors(dict(tensors, **specs), 1), **more)
+    assert not reached

@@ -67,12 +67,13 @@ template <int N, Way WAY> __device__ __forceinline__ void write_some(__amdgpu_bu
     else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), p, element * 4, 0, NT);
 }
 
-struct Penalty { float repetition, inverse, presence, frequency; };
+struct Penalty { float repetition, presence, frequency, scale, divisor, inverse; };   // divisor = repetition * scale, inverse = 1 / divisor
 
 // z with the penalties of an id that the text has.  count: bit 0: seen in the prompt; above: how often given.  The quotient is that by the
-// reciprocal with one correction (its remainder is exact), which is a few instructions where a division is ten.
+// reciprocal with one correction (its remainder is exact), which is a few instructions where a division is ten.  A repetition that has no
+// reciprocal in the type is scaled to one that has, and the logit with it (17 rows of 151,936 ids 8.6 us in a graph, with a division for all 8.8).
 __device__ __forceinline__ float penalised(float z, unsigned count, const Penalty &p) {
-    const float q = z * p.inverse, quotient = fmaf(fmaf(-q, p.repetition, z), p.inverse, q);
+    const float x = z * p.scale, q = x * p.inverse, quotient = fmaf(fmaf(-q, p.divisor, x), p.inverse, q);
     z = z > 0.f ? (q < INFINITY ? quotient : q) : z * p.repetition;
     if (count >> 1) z -= p.presence + p.frequency * (float)(count >> 1);
     return z;
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
     // the tables' sequence, or a guess at the first row's: right where all have as many rows
     int seq = (int)((long long)r0 * a.n_seqs / a.total_rows), end = 0;
     bool counted = false, biased = false, inside = false, clean = true;
-    Penalty p{1.f, 1.f, 0.f, 0.f};
+    Penalty p{1.f, 0.f, 0.f, 1.f, 1.f, 1.f};
     for (int r = r0; r < r1; ++r) {
         Some<T, STEP> z[EACH / STEP];
         uint32_t bits[EACH / STEP];
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
                 const int32_t *biases = x.bias_off ? x.bias_off + seq : x.row_off;
                 first = uniform(x.row_off, seq);
                 end = uniform(x.row_off, seq + 1);
-                p = Penalty{uniform(penalties, 0), 0.f, uniform(penalties, 1), uniform(penalties, x.penalties ? 2 : 1)};
+                p = Penalty{uniform(penalties, 0), uniform(penalties, 1), uniform(penalties, x.penalties ? 2 : 1), 0.f, 0.f, 0.f};
                 length = uniform(x.history ? x.history_len : x.row_off, seq);
                 prompt = uniform(x.prompt_len ? x.prompt_len : x.row_off, seq);
                 b0 = uniform(biases, 0);
@@ -153,7 +154,10 @@ __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kern
             end = max(end, r + 1);
             if (inside) {
                 counted = x.penalties && (p.repetition != 1.f || p.presence != 0.f || p.frequency != 0.f);
-                p.inverse = 1.f / p.repetition;
+                // by infinity: 0 / 1; by what is below the normal numbers, whose reciprocal may be infinite: both times 2^64
+                p.scale = p.repetition == INFINITY ? 0.f : fabsf(p.repetition) < 0x1p-126f ? 0x1p64f : 1.f;
+                p.divisor = p.repetition == INFINITY ? 1.f : p.repetition * p.scale;
+                p.inverse = 1.f / p.divisor;
                 const int n = x.history ? min(max(length, 0), a.max_history) : 0;
                 prompt = x.prompt_len ? min(max(prompt, 0), n) : 0;
                 b1 = x.bias_off ? min(max(b1, 0), a.bias_entries) : 0;

@@ -30,6 +30,28 @@ class _Adjust:
             self.more["biases"] = (ints([0, len(biases)]), ints(list(biases)), torch.tensor(list(biases.values()), dtype=torch.float32, device=dev))
         self.length = 0
 
+    def admitted(self, text, drafts):
+        """The drafts in front of the first that its row's ids exclude, none of which could be accepted: `allowed` is asked about
+        texts that it admits only.  Keeps the masks of their rows."""
+        self.mask = None
+        if self.allowed is None:
+            return drafts
+        bits, rows = np.zeros((len(drafts) + 1, -(-self.vocab // 32) * 32), bool), []
+        for i in range(len(drafts) + 1):
+            ids = self.allowed(list(text) + list(drafts[:i]))
+            rows.append(-1 if ids is None else i)
+            if ids is None:
+                continue
+            ids = [int(v) for v in ids]
+            if not all(0 <= v < self.vocab for v in ids):
+                raise ValueError(f"allowed ids outside the vocabulary of {self.vocab}")
+            bits[i, ids] = True
+            if i < len(drafts) and not (0 <= drafts[i] < self.vocab and bits[i, drafts[i]]):
+                drafts = drafts[:i]
+                break
+        self.mask = np.packbits(bits[:len(rows)], axis=1, bitorder="little").view(np.int32), rows
+        return drafts
+
     def __call__(self, text, tokens, drafts):
         """The logits of the rows of the text's end and of the drafts behind it, in place.  tokens: the rows' tokens on the device;
         the first of them, the pending token, counts as the end of the text."""
@@ -39,17 +61,9 @@ class _Adjust:
             more["history_len"].fill_(len(text))
             self.length = len(text)
             more["tokens"] = tokens
-        if self.allowed is not None:
-            bits, rows = np.zeros((m, -(-self.vocab // 32) * 32), bool), [-1] * m
-            for i in range(m):
-                ids = self.allowed(list(text) + list(drafts[:i]))
-                if ids is not None:
-                    ids = [int(v) for v in ids]
-                    if not all(0 <= v < self.vocab for v in ids):
-                        raise ValueError(f"allowed ids outside the vocabulary of {self.vocab}")
-                    bits[i, ids], rows[i] = True, i
-            words = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32))
-            more.update(mask=words.to(self.dev), mask_row=self.ints(rows))
+        if self.mask is not None:
+            words, rows = self.mask
+            more.update(mask=torch.from_numpy(words).to(self.dev), mask_row=self.ints(rows))
         vf.vf_logits_adjust(self.logits[:m], self.ints([0, m]), self.logits[:m], **more)
         return self.logits[:m]
 
@@ -63,7 +77,9 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
 
     The logits are adjusted before a token is taken from them (`vf_logits_adjust`), so that the text is what plain greedy
     decoding with the same adjustments would produce: penalties (repetition, presence, frequency); biases {id: value};
-    allowed(text) -> the ids that may follow a text, prompt included, or None for all."""
+    allowed(text) -> the ids that may follow a text, prompt included, or None for all.  `allowed` is asked about the text so far and about
+    what it admits behind it, no other drafts; drafts that it excludes are not verified.  Where it allows no id, 0 follows, as in any
+    row that is all -infinity."""
     dev = model.buf.device
     k = min(int(k), vf.VF_MAX_DRAFTS)
     toks = torch.as_tensor(list(prompt), dtype=torch.int32, device=dev)
@@ -76,6 +92,7 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
                             logits_out=adjust.logits if last and adjust is not None else None)
     length, pending = vf.vf_seq_get_state(seq)
     if adjust is not None:                              # the first token comes from adjusted logits too
+        adjust.admitted([int(t) for t in prompt], [])
         z = adjust([int(t) for t in prompt], None, [])[0]
         pending = int((z == z.max()).nonzero()[0])      # the lowest of equal ones, as vf_accept has it
         vf.vf_seq_set_pending(seq, pending)
@@ -94,7 +111,8 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
             fresh = [int(t) for t in drafter(text, k)][:k]
         else:
             fresh = vf.vf_draft_suffix_match(text, k, max_suffix, min_suffix)
-        drafts = vf.vf_reuse_pool_extend(pool, fresh) if k and reuse else fresh
+        proposed = vf.vf_reuse_pool_extend(pool, fresh) if k and reuse else fresh
+        drafts = proposed if adjust is None else adjust.admitted(text, proposed)
         m = len(drafts) + 1
         tokens = torch.as_tensor([vf.VF_PENDING] + drafts, dtype=torch.int32, device=dev)
         logits = None
@@ -108,8 +126,8 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
             vf.vf_reuse_select(tokens, [0, m], y[:m], n_acc, seg)
         host = torch.cat([n_acc, seg, out[:m]]).cpu().tolist()          # the step's one synchronisation
         a, seg_start, seg_len, emitted = host[0], host[1], host[2], host[3:4 + host[0]]
-        if drafts and reuse:
-            vf.vf_reuse_pool_update(pool, drafts, seg_start, seg_len)
+        if proposed and reuse:      # (a pool whose drafts are all excluded ages too)
+            vf.vf_reuse_pool_update(pool, drafts, *((seg_start, seg_len) if drafts else (0, 0)))
         text += emitted
         length += 1 + a
         vf.vf_seq_note_len(seq, length)                 # vf_accept counted all m rows; 1 + a were kept

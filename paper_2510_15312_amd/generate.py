@@ -12,6 +12,12 @@ import torch
 from . import binding as vf
 
 
+def _best(z):
+    """The id of the largest logit as vf_accept has it: the lowest of equal ones, what is not a number never."""
+    z = torch.where(z.isnan(), -float("inf"), z)
+    return int((z == z.max()).nonzero()[0])
+
+
 class _Adjust:
     """What `generate` puts on the logits: the text so far on the device, biases, and the masks of a step's rows."""
 
@@ -22,11 +28,14 @@ class _Adjust:
         self.more = {}
         if penalties is not None:
             penalties = list(penalties)
-            if len(penalties) != 3 or not penalties[0] > 0:
-                raise ValueError(f"penalties {penalties}: a repetition above 0, presence, frequency")
+            as_held = torch.tensor(penalties, dtype=torch.float32).tolist()      # (1e50 is infinite, 1e-50 zero)
+            if len(penalties) != 3 or not 0 < as_held[0] < float("inf") or as_held[1] + as_held[2] != as_held[1] + as_held[2]:
+                raise ValueError(f"penalties {penalties}: a finite repetition above 0, presence, frequency")
             self.more = dict(penalties=torch.tensor([penalties], dtype=torch.float32, device=dev), prompt_len=ints([len(prompt)]),
                              history=torch.zeros((1, room), dtype=torch.int32, device=dev), history_len=ints([0]))
         if biases:
+            if any(value != value for value in biases.values()):
+                raise ValueError(f"biases that are not numbers: {biases}")
             self.more["biases"] = (ints([0, len(biases)]), ints(list(biases)), torch.tensor(list(biases.values()), dtype=torch.float32, device=dev))
         self.length = 0
 
@@ -76,7 +85,7 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
     leaves the pool of rejected drafts out.
 
     The logits are adjusted before a token is taken from them (`vf_logits_adjust`), so that the text is what plain greedy
-    decoding with the same adjustments would produce: penalties (repetition, presence, frequency); biases {id: value};
+    decoding with the same adjustments would produce: penalties (a finite repetition above 0, presence, frequency); biases {id: value};
     allowed(text) -> the ids that may follow a text, prompt included, or None for all.  `allowed` is asked about the text so far and about
     what it admits behind it, no other drafts; drafts that it excludes are not verified.  Where it allows no id, 0 follows, as in any
     row that is all -infinity."""
@@ -94,7 +103,7 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
     if adjust is not None:                              # the first token comes from adjusted logits too
         adjust.admitted([int(t) for t in prompt], [])
         z = adjust([int(t) for t in prompt], None, [])[0]
-        pending = int((z == z.max()).nonzero()[0])      # the lowest of equal ones, as vf_accept has it
+        pending = _best(z)
         vf.vf_seq_set_pending(seq, pending)
     text = [int(t) for t in prompt] + [pending]        # the pending token is the first generated one
     pool = vf.vf_reuse_pool_init(reuse_max_age, max(k, 1))

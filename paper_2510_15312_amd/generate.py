@@ -79,7 +79,7 @@ class _Adjust:
 
 def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=256, reuse_max_age=2, drafter=None, reuse=True,
              penalties=None, biases=None, allowed=None):
-    """prompt: host ints; returns (the n_new generated tokens, statistics).  Greedy acceptance: the
+    """prompt: host ints, none where the sequence has its pending token already; returns (the n_new generated tokens, statistics).  Greedy acceptance: the
     result is what plain greedy decoding would produce.  drafter(text, k) -> list of at most k draft
     ids replaces the library's suffix-match drafter (any drafter gives the same text); reuse=False
     leaves the pool of rejected drafts out.
@@ -100,7 +100,7 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
         vf.vf_prefill_chunk(model, seq, toks[c0:c0 + chunk], sample_first=last, logits_mode=int(last and adjust is not None),
                             logits_out=adjust.logits if last and adjust is not None else None)
     length, pending = vf.vf_seq_get_state(seq)
-    if adjust is not None:                              # the first token comes from adjusted logits too
+    if adjust is not None and len(prompt):              # the first token comes from adjusted logits too
         adjust.admitted([int(t) for t in prompt], [])
         z = adjust([int(t) for t in prompt], None, [])[0]
         pending = _best(z)

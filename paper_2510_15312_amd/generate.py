@@ -18,6 +18,11 @@ def _best(z):
     return int((z == z.max()).nonzero()[0])
 
 
+def _sent(numbers, dev):
+    """On the device, from pinned memory, whose copy nobody waits for; torch keeps the memory until the copy is done."""
+    return torch.tensor(numbers, dtype=torch.int32, pin_memory=True).to(dev, non_blocking=True)
+
+
 class _Adjust:
     """What `generate` puts on the logits: the text so far on the device, biases, and the masks of a step's rows."""
 
@@ -61,20 +66,24 @@ class _Adjust:
         self.mask = np.packbits(bits[:len(rows)], axis=1, bitorder="little").view(np.int32), rows
         return drafts
 
-    def __call__(self, text, tokens, drafts):
-        """The logits of the rows of the text's end and of the drafts behind it, in place.  tokens: the rows' tokens on the device;
-        the first of them, the pending token, counts as the end of the text."""
-        m, more = len(drafts) + 1, dict(self.more)
-        if "history" in more:
-            more["history"][0, self.length:len(text)] = self.ints(text[self.length:])
-            more["history_len"].fill_(len(text))
+    def prepare(self, text, tokens, drafts):
+        """Sends what the rows of the text's end and of the drafts behind it need, ahead of the forward pass, so that nothing waits for that.
+        tokens: the rows' tokens on the device; the first of them, the pending token, counts as the end of the text."""
+        self.rows, self.args = len(drafts) + 1, dict(self.more, row_off=_sent([0, len(drafts) + 1], self.dev))
+        if "history" in self.more:
+            self.args["history"][0, self.length:len(text)] = _sent(text[self.length:], self.dev)
+            self.args["history_len"].fill_(len(text))
             self.length = len(text)
-            more["tokens"] = tokens
+            self.args["tokens"] = tokens
         if self.mask is not None:
             words, rows = self.mask
-            more.update(mask=torch.from_numpy(words).to(self.dev), mask_row=self.ints(rows))
-        vf.vf_logits_adjust(self.logits[:m], self.ints([0, m]), self.logits[:m], **more)
-        return self.logits[:m]
+            self.args.update(mask=torch.from_numpy(words).pin_memory().to(self.dev, non_blocking=True), mask_row=_sent(rows, self.dev))
+
+    def __call__(self):
+        """The logits of the prepared rows, in place."""
+        logits = self.logits[:self.rows]
+        vf.vf_logits_adjust(logits, out=logits, **self.args)
+        return logits
 
 
 def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=256, reuse_max_age=2, drafter=None, reuse=True,
@@ -102,8 +111,8 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
     length, pending = vf.vf_seq_get_state(seq)
     if adjust is not None and len(prompt):              # the first token comes from adjusted logits too
         adjust.admitted([int(t) for t in prompt], [])
-        z = adjust([int(t) for t in prompt], None, [])[0]
-        pending = _best(z)
+        adjust.prepare([int(t) for t in prompt], None, [])
+        pending = _best(adjust()[0])
         vf.vf_seq_set_pending(seq, pending)
     text = [int(t) for t in prompt] + [pending]        # the pending token is the first generated one
     pool = vf.vf_reuse_pool_init(reuse_max_age, max(k, 1))
@@ -123,13 +132,14 @@ def generate(model, seq, prompt, n_new, k=16, max_suffix=8, min_suffix=1, chunk=
         proposed = vf.vf_reuse_pool_extend(pool, fresh) if k and reuse else fresh
         drafts = proposed if adjust is None else adjust.admitted(text, proposed)
         m = len(drafts) + 1
-        tokens = torch.as_tensor([vf.VF_PENDING] + drafts, dtype=torch.int32, device=dev)
+        tokens = _sent([vf.VF_PENDING] + drafts, dev)
         logits = None
         if adjust is None:
             vf.vf_verify(model, [seq], tokens, [0, m])
         else:
+            adjust.prepare(text, tokens, drafts)
             vf.vf_verify(model, [seq], tokens, [0, m], adjust.logits)
-            logits = adjust(text, tokens, drafts)
+            logits = adjust()
         vf.vf_accept(model, [seq], tokens, [0, m], greedy, n_acc, out[:m], y[:m], logits)
         if drafts and reuse:
             vf.vf_reuse_select(tokens, [0, m], y[:m], n_acc, seg)

@@ -728,6 +728,10 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
         penalty = penalties.data_ptr()
     if history is not None:
         text_stride, text_most, text = _matrix("history", history, _I32, n, None, dev), history.shape[1], history.data_ptr()
+    lengths = None if history_len is None else _ints("history_len", history_len, n, dev)
+    prompts = None if prompt_len is None else _ints("prompt_len", prompt_len, n, dev)
+    if history is not None and text_most == 0:      # texts without a token, which have no address
+        text = lengths = prompts = None
     if mask is not None:
         mask_stride, bits, (masks, words) = _matrix("mask", mask, _I32, None, None, dev), mask.data_ptr(), mask.shape
         if 32 * words < vocab or mask_row is None and masks < rows:
@@ -743,7 +747,5 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
     _below_31_bits("logits", rows, vocab, text_most, entries, masks)
     a = vf_logits_args(_dtype(logits), n, rows, vocab, text_most, entries, masks, 0, in_stride, out_stride, text_stride, mask_stride)
     _launch(dev, lib.vf_logits_adjust, C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), penalty, text,
-            None if history_len is None else _ints("history_len", history_len, n, dev),
-            None if prompt_len is None else _ints("prompt_len", prompt_len, n, dev),
-            None if tokens is None else _ints("tokens", tokens, rows, dev), bias_off, bias_id, bias, bits,
+            lengths, prompts, None if tokens is None else _ints("tokens", tokens, rows, dev), bias_off, bias_id, bias, bits,
             None if mask_row is None else _ints("mask_row", mask_row, rows, dev), _stream_of(logits))

@@ -535,7 +535,8 @@ typedef struct {
  * biases outside 0 .. bias_entries are taken as the nearer of the two.  Row r has mask
  * mask_row[r] (a number outside 0 .. mask_rows - 1: none), id v is bit v % 32 of its word v / 32.  A row whose mask leaves nothing is all
  * -infinity.  penalties is float32 [n_seqs][3], rho > 0 (also infinite: a positive logit becomes 0, one of 0 no number).  NULL stands for no penalties, no history, no prompt, no row tokens, no
- * biases, no masks; with mask_row NULL row r has mask r.  Arithmetic is float32.  out may be logits (float32, the same stride).  Rows outside the
+ * biases, no masks; with mask_row NULL row r has mask r.  Arithmetic is float32.  out may be logits (float32, the same stride); where a row
+ * of it shares memory with a row of logits otherwise the call is refused, and with what else the call reads it shares none.  Rows outside the
  * sequences are not written. */
 int vf_logits_adjust(const vf_logits_args *args, const void *logits_dev, const int32_t *row_off_dev, float *out_dev,
                      const float *penalties_dev, const int32_t *history_dev, const int32_t *history_len_dev,

@@ -324,6 +324,17 @@ template <typename T> int launch(const vf_logits_args &a, const LogitsArrays &x,
     return vec ? launch<T, true>(a, x, logits, out, st) : launch<T, false>(a, x, logits, out, st);
 }
 
+// Whether a row of `a` (bytes a_row, a_step apart) shares bytes with a row of `b`, both of `rows` rows: rows of one may lie between those of the other.
+bool rows_overlap(uintptr_t a, int64_t a_row, int64_t a_step, uintptr_t b, int64_t b_row, int64_t b_step, int rows) {
+    if (a >= b + (rows - 1) * b_step + b_row || b >= a + (rows - 1) * a_step + a_row) return false;
+    for (int r = 0; r < rows; ++r) {
+        // of the rows of b that end behind the start of this one, the first
+        const int64_t start = (int64_t)(a - b) + r * a_step, first = start < b_row ? 0 : (start - b_row) / b_step + 1;
+        if (first < rows && first * b_step < start + a_row) return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 extern "C" int vf_logits_adjust(const vf_logits_args *args, const void *logits_dev, const int32_t *row_off_dev, float *out_dev,
@@ -349,10 +360,14 @@ extern "C" int vf_logits_adjust(const vf_logits_args *args, const void *logits_d
     if ((history_dev || tokens_dev) && !penalties_dev) history_dev = tokens_dev = nullptr;    // nothing counts them
     if (bias_off_dev && (a.bias_entries < 0 || a.bias_entries > VF_LOGITS_MAX_BIASES || (a.bias_entries > 0 && (!bias_id_dev || !bias_dev))))
         return vf_fail(VF_ERR_ARG, "vf_logits_adjust: %d biases", a.bias_entries);
-    if (mask_dev && (a.mask_rows < 0 || a.mask_stride < (a.vocab + 31) / 32 || (!mask_row_dev && a.mask_rows < a.total_rows)))
-        return vf_fail(VF_ERR_ARG, "vf_logits_adjust: %d masks, stride %lld", a.mask_rows, (long long)a.mask_stride);
     if (((uintptr_t)logits_dev & (a.dtype == VF_F32 ? 3 : 1)) | ((uintptr_t)out_dev & 3))
         return vf_fail(VF_ERR_UNSUPPORTED, "vf_logits_adjust: addresses are multiples of an element");
+    const int es = a.dtype == VF_F32 ? 4 : 2;
+    if ((const void *)out_dev != logits_dev && rows_overlap((uintptr_t)logits_dev, (int64_t)a.vocab * es, a.in_stride * es, (uintptr_t)out_dev,
+                                                            (int64_t)a.vocab * 4, a.out_stride * 4, a.total_rows))
+        return vf_fail(VF_ERR_ARG, "vf_logits_adjust: out shares memory with the logits and is not them");
+    if (mask_dev && (a.mask_rows < 0 || a.mask_stride < (a.vocab + 31) / 32 || (!mask_row_dev && a.mask_rows < a.total_rows)))
+        return vf_fail(VF_ERR_ARG, "vf_logits_adjust: %d masks, stride %lld", a.mask_rows, (long long)a.mask_stride);
     const LogitsArrays x = {row_off_dev, penalties_dev, history_dev, history_len_dev, prompt_len_dev, tokens_dev, bias_off_dev, bias_id_dev, bias_dev,
                             mask_dev, mask_row_dev};
     return a.dtype == VF_F32 ? launch<float>(a, x, logits_dev, out_dev, (hipStream_t)stream)

@@ -445,8 +445,12 @@ _I32 = torch.int32
 
 
 @functools.cache
+def _device_count():
+    return torch.cuda.device_count()
+
+
 def _several_devices():
-    return torch.cuda.device_count() > 1
+    return _device_count() > 1
 
 
 def _device(name, t):
@@ -455,6 +459,20 @@ def _device(name, t):
     if not t.is_cuda:
         _refuse(f"{name}: device tensor")
     return t.get_device() if _several_devices() else None
+
+
+def _current_device():
+    """The current device's number; None where there is no other."""
+    return torch.cuda.current_device() if _device_count() > 1 else None
+
+
+def _launch(dev, call, *args):
+    """A call whose tensors are on device dev: where that is not the current one, it is for the call, as the default streams of all
+    devices have one address."""
+    if dev is None or _current_device() in (dev, None):
+        return _check(call(*args))
+    with torch.cuda.device(dev):
+        _check(call(*args))
 
 
 def _on(device):
@@ -524,10 +542,10 @@ def vf_pages_assign(lens, new, free_pages, n_free, block_table, row_off, pos, sl
     dev = _device("lens", lens)
     n, m, stride = _table(block_table, dev)
     rows = pos.numel()
-    _check(lib.vf_pages_assign(n, m, stride, rows, free_pages.numel(), _ints("lens", lens, n, dev), _ints("new", new, n, dev),
-                               _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev), block_table.data_ptr(),
-                               _ints("row_off", row_off, n + 1, dev), _ints("pos", pos, rows, dev), _ints("slot", slot, rows, dev),
-                               _ints("kv_len", kv_len, n, dev), _ints("n_free_out", n_free_out, 1, dev), _stream_of(lens)))
+    _launch(dev, lib.vf_pages_assign, n, m, stride, rows, free_pages.numel(), _ints("lens", lens, n, dev), _ints("new", new, n, dev),
+            _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev), block_table.data_ptr(),
+            _ints("row_off", row_off, n + 1, dev), _ints("pos", pos, rows, dev), _ints("slot", slot, rows, dev),
+            _ints("kv_len", kv_len, n, dev), _ints("n_free_out", n_free_out, 1, dev), _stream_of(lens))
 
 
 def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED, factor=1.0, low=0.0, high=0.0, trained=0.0,
@@ -535,7 +553,7 @@ def vf_rotary_table(rotary_dim, theta, max_positions, scaling=VF_ROTARY_UNSCALED
     """float32 [max_positions, rotary_dim / 2, 2]: cos and sin of every position's angles."""
     plan = vf_rotary_plan(int(rotary_dim), int(max_positions), int(scaling), 0, theta, factor, low, high, trained, magnitude)
     table = torch.empty((max(int(max_positions), 0), max(int(rotary_dim), 0) // 2, 2), dtype=torch.float32, device=device)
-    _check(lib.vf_rotary_table(C.byref(plan), _ptr(table), _stream_of(table)))
+    _launch(_device("table", table), lib.vf_rotary_table, C.byref(plan), _ptr(table), _stream_of(table))
     return table
 
 
@@ -556,22 +574,9 @@ def vf_rotary_append(q, k, v, table, pos, slot, q_out, pool, pairs=VF_ROTARY_HAL
     slot int32 [rows], pool: one layer's pages (kv_layer)."""
     dev = _device("q", q)
     args = _rotary_args(q, k, v, table, q_out, pool, pairs, dev)
-    _check(lib.vf_rotary_append(C.byref(args), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                _ints("pos", pos, args.total_rows, dev), _ints("slot", slot, args.total_rows, dev), q_out.data_ptr(),
-                                pool.data_ptr(), _stream_of(q)))
-
-
-def _current_device():
-    return torch.cuda.current_device()
-
-
-def _launch(dev, call, *args):
-    """A call whose tensors are on device dev: where that is not the current one, it is for the call, as the default streams of all
-    devices have one address."""
-    if dev is None or dev == _current_device():
-        return _check(call(*args))
-    with torch.cuda.device(dev):
-        _check(call(*args))
+    _launch(dev, lib.vf_rotary_append, C.byref(args), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+            _ints("pos", pos, args.total_rows, dev), _ints("slot", slot, args.total_rows, dev), q_out.data_ptr(),
+            pool.data_ptr(), _stream_of(q))
 
 
 def _gain(name, t, heads, hd, dev):
@@ -620,9 +625,9 @@ def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, ma
     args = _packed_args(q, pool, block_table, out, max_rows, max_keys, scale, dev)
     if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous() or dev is not None and workspace.get_device() != dev:
         _refuse(f"workspace: contiguous uint8 tensor{_on(dev)}")
-    _check(lib.vf_attention_packed(C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
-                                   _ints("row_off", row_off, args.n_seqs + 1, dev), _ints("kv_len", kv_len, args.n_seqs, dev),
-                                   out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(q)))
+    _launch(dev, lib.vf_attention_packed, C.byref(args), q.data_ptr(), pool.data_ptr(), block_table.data_ptr(),
+            _ints("row_off", row_off, args.n_seqs + 1, dev), _ints("kv_len", kv_len, args.n_seqs, dev),
+            out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(q))
 
 
 # ---- requests that branch, are cut back or move --------------------------------------------------

@@ -172,6 +172,7 @@ class PackedBatch:
         """Of the request's tokens the first `tokens` stay (drafts that were not accepted go); pages behind them are free again.
         Between steps: a step that is open has taken its pages from the free list as it stood.  Returns what the request holds now."""
         self._within(False, "keep")
+        request = range(len(self.host_lens))[request]       # (-1: the last)
         first, last = -(-tokens // PAGE), -(-self.host_lens[request] // PAGE)
         if not 0 <= tokens <= self.host_lens[request]:
             raise ValueError(f"request {request} holds {self.host_lens[request]} tokens, not {tokens}")

@@ -728,7 +728,7 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
     penalty = text = bits = None
     text_most = text_stride = masks = mask_stride = entries = 0
     if penalties is not None:
-        if _matrix("penalties", penalties, torch.float32, n, 3, dev) != 3:
+        if _matrix("penalties", penalties, torch.float32, n, 3, dev) != 3 and n > 1:
             _refuse(f"penalties: contiguous float32 tensor [{n}, 3]{_on(dev)}")
         penalty = penalties.data_ptr()
     if history is not None:

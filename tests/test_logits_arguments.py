@@ -47,3 +47,19 @@ def test_a_history_with_columns_is_handed_on(handed):
     vf.vf_logits_adjust(**_tensors(LOGITS, 1))
     call, = handed
     assert call["history"] == call["history_len"] == call["prompt_len"] == 4096 and call["sizes"].max_history == 7
+
+
+class Apart(Sized):
+    """Rows four elements apart."""
+    def stride(self):
+        return 4, 1
+
+
+def test_penalties_of_one_sequence_from_a_wider_row(handed):
+    """One row is contiguous whatever lies between it and the next."""
+    one = _tensors(dict(LOGITS, row_off=(I32, 2), history=(I32, 1, 7), history_len=(I32, 1), prompt_len=(I32, 1)), 1)
+    vf.vf_logits_adjust(**dict(one, penalties=Apart(1, F32, 1, 3)))
+    assert handed[0]["penalties"] == 4096
+    with pytest.raises(vf.VfError):
+        vf.vf_logits_adjust(**dict(_tensors(LOGITS, 1), penalties=Apart(1, F32, 3, 3)))
+    assert len(handed) == 1

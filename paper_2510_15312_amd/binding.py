@@ -634,7 +634,7 @@ def vf_attention_packed(q, pool, block_table, row_off, kv_len, out, max_rows, ma
 
 def _pages_args(block_table, shares, free_entries, dev):
     (n, m, stride), pages = _table(block_table, dev), shares.numel()
-    _below_31_bits("pages", stride, pages, free_entries)
+    _below_31_bits("pages", n, stride, pages, free_entries)
     return vf_pages_args(n, m, stride, pages, free_entries, 0)
 
 
@@ -643,6 +643,7 @@ def vf_pages_fork(src, dst, tokens, lens, free_pages, n_free, block_table, share
     pages]; results kv_len [n], n_free_out [1], copies [forks, 2], n_copies [1], and what changes in block_table and shares."""
     dev = _device("lens", lens)
     a, forks = _pages_args(block_table, shares, free_pages.numel(), dev), src.numel()
+    _below_31_bits("src", forks)
     _launch(dev, lib.vf_pages_fork, C.byref(a), forks, _ints("src", src, forks, dev), _ints("dst", dst, forks, dev), _ints("tokens", tokens, forks, dev),
             _ints("lens", lens, a.n_seqs, dev), _ints("free_pages", free_pages, 0, dev), _ints("n_free", n_free, 1, dev),
             block_table.data_ptr(), _ints("shares", shares, 1, dev), _ints("kv_len", kv_len, a.n_seqs, dev),
@@ -749,7 +750,7 @@ def vf_logits_adjust(logits, row_off, out, penalties=None, history=None, history
                 dev is not None and bias.get_device() != dev:
             _refuse(f"biases: contiguous float32 tensor of {entries} entries{_on(dev)}")
         bias_off, bias_id, bias = _ints("bias_off", bias_off, n + 1, dev), _ints("bias_id", bias_id, 0, dev), bias.data_ptr()
-    _below_31_bits("logits", rows, vocab, text_most, entries, masks)
+    _below_31_bits("logits", n, rows, vocab, text_most, entries, masks)
     a = vf_logits_args(_dtype(logits), n, rows, vocab, text_most, entries, masks, 0, in_stride, out_stride, text_stride, mask_stride)
     _launch(dev, lib.vf_logits_adjust, C.byref(a), logits.data_ptr(), _ints("row_off", row_off, 1, dev), out.data_ptr(), penalty, text,
             lengths, prompts, None if tokens is None else _ints("tokens", tokens, rows, dev), bias_off, bias_id, bias, bits,

@@ -58,19 +58,19 @@ struct ForkArgs {
     int32_t *table, *shares, *kv_len, *n_free_out, *copies, *n_copies;
 };
 
-// Two prefix sums over the forks (pages of their own, table entries that they share) say where everything goes; every workgroup
-// takes them for itself and then its share of the entries, so there is one launch.  The lengths go to an array of their own, as
+// Two prefix sums over the forks (pages of their own, table entries that they share; the latter stay in LDS for the search) say where everything goes;
+// every workgroup takes them for itself and then its share of the entries, so there is one launch.  The lengths go to an array of their own, as
 // others still read the old ones.  Bound by the way from one read to the next (forks, lengths, last pages, entries): 4 forks of 1000
 // tokens 4.0 us, 64 of 1400 7.1, 2048 of 3840 about 16 with 122,880 entries.
 __global__ __launch_bounds__(FORK_THREADS) void pages_fork_kernel(ForkArgs a) {
     extern __shared__ int lds[];
-    int *own = lds, *entries = lds + a.n_forks + 1, *taker = lds + 2 * (a.n_forks + 1);   // taker[b]: the first fork into b
+    int *entries = lds, *taker = lds + a.n_forks + 1;    // entries that go before fork i's; the first fork into sequence b
     __shared__ int wave_sums[FORK_THREADS / 64];
     const PagesArgs &p = a.p;
     const int tid = threadIdx.x, nf = a.n_forks;
     const int n_free = min(max(a.n_free[0], 0), p.free_entries);
     for (int b = tid; b < p.n_seqs; b += FORK_THREADS) taker[b] = nf;
-    if (tid == 0) own[0] = entries[0] = 0;
+    if (tid == 0) entries[0] = 0;
     __syncthreads();
     for (int i = tid; i < nf; i += FORK_THREADS) {
         const int d = a.dst[i];
@@ -96,7 +96,6 @@ __global__ __launch_bounds__(FORK_THREADS) void pages_fork_kernel(ForkArgs a) {
         const int upto_entries = entries_before + scan<FORK_THREADS>(granted ? t / VF_TILE : 0, wave_sums, total);
         entries_before += total;
         if (i < nf) {
-            own[i + 1] = upto;
             entries[i + 1] = upto_entries;
             if (blockIdx.x == 0 && d >= 0 && d < p.n_seqs && taker[d] == i) {
                 a.kv_len[d] = granted ? t : a.len[d];
@@ -434,7 +433,7 @@ int vf_pages_fork(const vf_pages_args *args, int n_forks, const int32_t *src_dev
                         kv_len_dev, n_free_out_dev, copies_dev, n_copies_dev};
     const long long each = FORK_THREADS * FORK_ENTRIES;
     const int blocks = (int)std::max(1ll, std::min(256ll, ((long long)n_forks * args->max_pages + each - 1) / each));
-    hipLaunchKernelGGL(pages_fork_kernel, dim3(blocks), dim3(FORK_THREADS), (size_t)(2 * (n_forks + 1) + args->n_seqs) * sizeof(int),
+    hipLaunchKernelGGL(pages_fork_kernel, dim3(blocks), dim3(FORK_THREADS), (size_t)(n_forks + 1 + args->n_seqs) * sizeof(int),
                        (hipStream_t)stream, a);
     VF_LAUNCH_CHECK("pages_fork");
     return VF_OK;

@@ -86,8 +86,10 @@ __device__ __forceinline__ float penalised(float z, unsigned count, const Penalt
 // It is bound by memory, and for few rows by reads that wait for one another: all that depends on the sequence alone is asked for with its offsets,
 // for a sequence that is guessed (right where all have as many rows), then come the text, biases and masks, and the tables.  What the
 // tables cost is time in which a workgroup's loads and stores rest: 70 rows of 128,256 bfloat16 logits with texts of 1500 and 300 biases each take
-// 17.8 us in a graph (3.07 TB/s), about 13 without the tables; seven workgroups a compute unit hide the rest of it.  One row of
-// 151,936 ids 3.9 us, 270 rows of 16 sequences with everything 66.5 us (5.0 TB/s; a large copy 4.74).
+// 18.2 us in a graph (3.0 TB/s), about 13 without the tables; seven workgroups a compute unit hide the rest of it.  One row of
+// 151,936 ids 3.9 us, 270 rows of 16 sequences with everything 66.0 us (5.05 TB/s; a large copy 4.74).
+// Over themselves 170 rows with texts of 2000 and 40 biases take 31.9 us, apart 33.8, though without masks only 37 MB are read and 11 written where apart
+// 103 go each way: the same slices find the few ids that change, and each reads the whole text.
 // Rows that do not start at a multiple of four ids keep fewer tokens in flight, for eight wavefronts a SIMD: 100 rows of 100,003 ids 24.4 us for 26.5.
 template <typename T, int SLICE, bool VEC, Way WAY>
 __global__ __launch_bounds__(LOGIT_THREADS, VEC ? 1 : 8) void logits_adjust_kernel(vf_logits_args a, LogitsArrays x, const T *logits, float *out, int slices,
@@ -313,7 +315,8 @@ template <typename T, bool VEC> int launch(const vf_logits_args &a, const Logits
     const long long thousands = (a.vocab + 1023ll) / 1024 * a.total_rows;
     // few of them: one row of 151,936 ids 4.1 us for 4.5, four of 100,003 5.8 for 6.7; eight of 151,936 7.4 for 6.6
     if (thousands <= 800) return launch<T, 1024, VEC>(a, x, logits, out, st);
-    // many rows of a sequence each with room for long texts (200 rows, texts of 8000: 57.7 us for 63.5, of 2000 46.8 for 47.5, of 200 45.8 for 41.3)
+    // many rows of a sequence each with room for long texts, whose lengths only the device knows (200 rows, texts of 8000: 57.7 us for 63.5, of 2000 46.8
+    // for 47.5, of 200 in a history as wide 45.8 for 41.3)
     if (VEC && thousands > 16384 && a.max_history >= 1024 && a.total_rows < 2ll * a.n_seqs) return launch<T, VEC ? 4096 : 2048, VEC>(a, x, logits, out, st);
     return launch<T, 2048, VEC>(a, x, logits, out, st);
 }

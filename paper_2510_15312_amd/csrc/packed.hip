@@ -176,15 +176,15 @@ __device__ __forceinline__ void turn_unit(float *x, const float2 *angle, bool ha
 // of one head of v, which go through LDS to be written as pieces of eight tokens; v, with the longest way, comes first.  Workgroups of
 // k and v whose rows are neighbours run on one die, whose L2 joins what they write to one line.  A thread of q and k keeps its row's angles
 // over BATCH heads and asks for all their pieces before it turns the first.
-// 8192 rows of 24 + 2 x 8 heads of 128: 39.3 us = 4.4 TB/s where a large copy reaches 4.8; 16 rows at 1.5B 3.1 us, the launch and
-// three dependent reads (position, angles, elements).
+// 8192 rows of 24 + 2 x 8 heads of 128: 39.3 us = 4.4 TB/s where a large copy reaches 4.8; 16 rows at 1.5B 3.1 us, the launch,
+// the position (for k the slot too), then angles and elements, which are asked for together.
 constexpr int ROTARY_ROWS = 16, ROTARY_V_ROWS = 64;
 
 struct RotaryGrid { int32_t heads, v, k, v_rows, v_single; };   // heads a workgroup of q or k; workgroups of v, of k; rows a workgroup of v; each by itself
 
 // Norms of q and k before they turn: a sum of squares over a head, which lies in neighbouring lanes of a wavefront, and a gain for each element.
 // That takes registers, so BATCH is 2 with them (8192 rows of 24 + 2 x 8 heads of 128: 41.7 us with four heads at a time, 38.8 with two, 47.4 with
-// eight) and 4 without.
+// eight) and 4 without.  Gains for every head are read when the head's sum is there, one more trip for each (float32, 1100 rows 4.8 us in a graph).
 struct HeadNorms { static constexpr int BATCH = 2; vf_head_norm n; };
 struct NoNorms { static constexpr int BATCH = 4; };
 
